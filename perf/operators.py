@@ -241,12 +241,12 @@ def _own(s, case, kind):
     from paper_2310_10537_amd import binding as mx
     fmts = {"e4m3": mx.FP8_E4M3, "e5m2": mx.FP8_E5M2}
     if kind == "norm":
-        h = torch.empty_like(s["x"]) if case["residual"] else None
+        h = _rows_of(case["rows"], case["cols"], s["x"].dtype) if case["residual"] else None
         e, sc = mx.mx_rmsnorm_b128(s["x"], s["w"], EPS, fmts[case["fmt"]], residual=s["r"], h_out=h)
         values = mx.mx_dequantize_b128(e, sc, fmts[case["fmt"]], case["rows"], case["cols"], 1, out=_rows_of(case["rows"], case["cols"], torch.bfloat16))
         return (h, values) if case["residual"] else values
     if kind == "projection":
-        h = torch.empty_like(s["x"]) if case["residual"] else None
+        h = _rows_of(case["rows"], case["cols"], s["x"].dtype) if case["residual"] else None
         fmt = fmts[case["fmt"]]
         e, sc = mx.mx_rmsnorm_q(s["x"], s["w"], EPS, fmt, residual=s["r"], h_out=h)
         c = mx.mx_gemm(e, sc, fmt, *s["b"], mx.FP8_E4M3, case["cols"], dtype=torch.bfloat16)
