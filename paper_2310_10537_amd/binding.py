@@ -1,4 +1,4 @@
-"""ctypes binding of libmx.so (C ABI in include/mx.h).
+"""ctypes binding of libmx.so (C ABI in include/mx.h, include/mx_b128.h, include/mx_norm.h).
 
 Argument marshalling only: every step of the cast, the dequantize and the GEMM
 runs in the HIP kernels of the library.  PyTorch is used for device memory and
@@ -64,6 +64,23 @@ def lib() -> ctypes.CDLL:
         L.mx_stream_pattern.argtypes = [vp, vp, i64, ci, ci, vp]
         L.mx_gemm_probe.argtypes = [i64, i64, i64, vp, vp, ci, vp, vp, ci, vp, i64, vp, i64, vp]
         L.mx_mfma_stream_probe.argtypes = [ci, vp, ci, vp, vp, vp]
+        cf = ctypes.c_float
+        L.mx_b128_elem_bytes.argtypes = [i64, i64, ci]
+        L.mx_b128_elem_bytes.restype = sz
+        L.mx_b128_scale_count.argtypes = [i64, i64, ci, ci]
+        L.mx_b128_scale_count.restype = sz
+        L.mx_quantize_b128.argtypes = [vp, ci, i64, i64, i64, ci, ci, ci, vp, vp, vp]
+        L.mx_dequantize_b128.argtypes = [vp, vp, ci, i64, i64, ci, ci, vp, ci, i64, vp]
+        L.mx_gemm_b128.argtypes = [i64, i64, i64, vp, vp, ci, ci, vp, vp, ci, ci, vp, ci, i64, vp]
+        norm = [vp, i64, vp, i64, vp, ci, ci, i64, i64, cf]
+        outs = [vp, i64, vp, i64, vp, vp]
+        L.mx_rmsnorm.argtypes = norm + outs
+        L.mx_rmsnorm_q.argtypes = norm + [ci, ci, vp, vp] + outs
+        L.mx_rmsnorm_b128.argtypes = norm + [ci, vp, vp] + outs
+        L.mx_rmsnorm_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.mx_rmsnorm_bwd_workspace_bytes.restype = sz
+        L.mx_rmsnorm_bwd.argtypes = [vp, i64, vp, i64, vp, ci, vp, vp, i64, ci, i64, i64, vp, i64, vp, vp]
+        L.mx_rmsnorm_bwd_ws.argtypes = [vp, i64, vp, i64, vp, ci, vp, vp, i64, ci, i64, i64, vp, i64, vp, vp, sz, vp]
         L.mx_strerror.argtypes = [ci]
         L.mx_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -411,3 +428,214 @@ def mx_dequantize_3d(elems, scales, fmt, shape, axis, keep_order=False, dtype=to
     _check(lib().mx_dequantize_3d(elems.data_ptr(), scales.data_ptr(), fmt, d0, d1, d2, axis, 1 if keep_order else 0,
                                   out.data_ptr(), _dt(out), s0, s1, _stream(stream)))
     return out
+
+
+# ---------------------------------------------------------------------------------------------
+# 8-bit floating point with a Float32 scale for each block of 128 (include/mx_b128.h)
+# ---------------------------------------------------------------------------------------------
+BLOCK128 = 128
+
+
+class _On:
+    """The device of a call's tensors made the current one, and the stream that the call runs on: the given one, else torch's current
+    stream of that device."""
+    __slots__ = ("guard", "stream")
+
+    def __init__(self, device, stream):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return ctypes.c_void_p(self.stream.cuda_stream)
+
+    def __exit__(self, *a):
+        if self.guard is not None:
+            self.guard.__exit__(*a)
+
+
+def _rows(t, name, like=None):
+    """Pitch (elements) of a 2-D float32 / bfloat16 device tensor whose rows are contiguous; `like`: it has that tensor's shape, type and device."""
+    _dev(t, name)
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} must have the shape {tuple(like.shape)}, type and device of the tensor it goes with")
+    if t.shape[0] > 1:
+        return t.stride(0)
+    per16 = 16 // t.element_size()
+    return -(-t.shape[1] // per16) * per16            # one row: its pitch is never used, but has to be a possible one
+
+
+def _flat(t, name, shape, dtype, device):
+    """A contiguous tensor of exactly this shape and type."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {device}")
+    return t
+
+
+def _b128_shapes(rows, cols, axis, tile):
+    lines, length = (rows, cols) if axis == 1 else (cols, rows)
+    blocks = -(-length // BLOCK128)
+    return (lines, blocks * BLOCK128), (-(-lines // BLOCK128) if tile else lines, blocks)
+
+
+def mx_quantize_b128(src, axis, fmt, tile=False, elems_out=None, scales_out=None, stream=None):
+    """src: 2-D device tensor (float32 / bfloat16, rows contiguous).  Returns (elems uint8 [lines, 128 blocks],
+    scales float32 [lines, blocks], or [lines / 128, blocks] with tile): blocks of 128 along `axis`, or 128 x 128 tiles."""
+    ld = _rows(src, "src")
+    dt = _dt(src)
+    rows, cols = src.shape
+    shape_e, shape_s = _b128_shapes(rows, cols, axis, tile)
+    elems = torch.empty(shape_e, dtype=torch.uint8, device=src.device) if elems_out is None else _flat(elems_out, "elems_out", shape_e, torch.uint8, src.device)
+    scales = torch.empty(shape_s, dtype=torch.float32, device=src.device) if scales_out is None else _flat(scales_out, "scales_out", shape_s, torch.float32, src.device)
+    with _On(src.device, stream) as st:
+        _check(lib().mx_quantize_b128(src.data_ptr(), dt, rows, cols, ld, axis, 1 if tile else 0, fmt, elems.data_ptr(), scales.data_ptr(), st))
+    return elems, scales
+
+
+def mx_dequantize_b128(elems, scales, fmt, rows, cols, axis, tile=False, dtype=torch.float32, out=None, stream=None):
+    """Returns the row-major [rows, cols] tensor of elems * scales (axis and tile as cast)."""
+    _dev(elems, "elems")
+    shape_e, shape_s = _b128_shapes(rows, cols, axis, tile)
+    _flat(elems, "elems", shape_e, torch.uint8, elems.device)
+    _flat(scales, "scales", shape_s, torch.float32, elems.device)
+    if out is None:
+        out = _empty_rows(rows, cols, dtype, elems.device)
+    elif tuple(out.shape) != (rows, cols) or out.device != elems.device:
+        raise ValueError(f"out must be a [{rows}, {cols}] tensor on {elems.device}")
+    ld = _rows(out, "out")
+    with _On(elems.device, stream) as st:
+        _check(lib().mx_dequantize_b128(elems.data_ptr(), scales.data_ptr(), fmt, rows, cols, axis, 1 if tile else 0, out.data_ptr(), _dt(out), ld, st))
+    return out
+
+
+def _empty_rows(rows, cols, dtype, device):
+    """A matrix whose rows start at multiples of 16 bytes."""
+    per16 = 16 // torch.empty((), dtype=dtype).element_size()
+    if cols % per16 == 0 or rows <= 1:
+        return torch.empty((rows, cols), dtype=dtype, device=device)
+    return torch.empty((rows, -(-cols // per16) * per16), dtype=dtype, device=device)[:, :cols]
+
+
+def _b128_operand(elems, scales, name, K):
+    """(lines, whether the scales are those of 128 x 128 tiles) of a product's operand."""
+    _dev(elems, name + "_elems")
+    if elems.dim() != 2 or elems.shape[1] != K or elems.dtype != torch.uint8 or not elems.is_contiguous():
+        raise ValueError(f"{name}_elems must be a contiguous uint8 tensor [lines, {K}]")
+    lines = elems.shape[0]
+    tile = scales.shape != (lines, K // BLOCK128)
+    _flat(scales, name + "_scales", (-(-lines // BLOCK128), K // BLOCK128) if tile else (lines, K // BLOCK128), torch.float32, elems.device)
+    return lines, tile
+
+
+def mx_gemm_b128(A_elems, A_scales, fmtA, B_elems, B_scales, fmtB, K, dtype=torch.float32, out=None, stream=None):
+    """C[M, N] = A[M, K] . B[N, K]^T on operands cast by mx_quantize_b128; which have 128 x 128 tiles is seen from their scales' shapes."""
+    M, tileA = _b128_operand(A_elems, A_scales, "A", K)
+    N, tileB = _b128_operand(B_elems, B_scales, "B", K)
+    if B_elems.device != A_elems.device:
+        raise ValueError("A and B must be on one device")
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=A_elems.device)
+    elif tuple(out.shape) != (M, N) or out.device != A_elems.device or (N > 1 and out.stride(1) != 1):
+        raise ValueError(f"out must be a [{M}, {N}] tensor with contiguous rows on {A_elems.device}")
+    ldc = out.stride(0) if M > 1 else N
+    with _On(A_elems.device, stream) as st:
+        _check(lib().mx_gemm_b128(M, N, K, A_elems.data_ptr(), A_scales.data_ptr(), tileA, fmtA, B_elems.data_ptr(), B_scales.data_ptr(), tileB, fmtB,
+                                  out.data_ptr(), _dt(out), ldc, st))
+    return out
+
+
+# ---------------------------------------------------------------------------------------------
+# RMS norm (include/mx_norm.h)
+# ---------------------------------------------------------------------------------------------
+def _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out):
+    """(the leading arguments of a norm call, the trailing ones)"""
+    ldx = _rows(x, "x")
+    rows, cols = x.shape
+    ldr = _rows(residual, "residual", x) if residual is not None else 0
+    ldh = _rows(h_out, "h_out", x) if h_out is not None else 0
+    ldy = _rows(y_out, "y_out", x) if y_out is not None else 0
+    w_dt = DT_F32
+    if weight is not None:
+        _flat(weight, "weight", (cols,), weight.dtype, x.device)
+        w_dt = _dt(weight)
+    if rstd_out is not None:
+        _flat(rstd_out, "rstd_out", (rows,), torch.float32, x.device)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    return ((x.data_ptr(), ldx, ptr(residual), ldr, ptr(weight), w_dt, _dt(x), rows, cols, float(eps)),
+            (ptr(h_out), ldh, ptr(y_out), ldy, ptr(rstd_out)))
+
+
+def mx_rmsnorm(x, weight, eps, residual=None, h_out=None, y_out=None, rstd_out=None, stream=None):
+    """y = h * weight / sqrt(mean(h^2) + eps) per row, h = x + residual, in x's type.  h_out (which may be x or residual) receives h,
+    rstd_out ([rows] float32) the factor that mx_rmsnorm_bwd wants.  Returns y."""
+    if y_out is None:
+        _rows(x, "x")
+        y_out = _empty_rows(x.shape[0], x.shape[1], x.dtype, x.device)
+    head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
+    with _On(x.device, stream) as st:
+        _check(lib().mx_rmsnorm(*head, *tail, st))
+    return y_out
+
+
+def mx_rmsnorm_q(x, weight, eps, fmt, rnd=ROUND_RNE, residual=None, h_out=None, y_out=None, rstd_out=None, elems_out=None, scales_out=None, stream=None):
+    """The norm delivered as an MX tensor blocked along the row: (elems, scales) as mx_quantize(y, 1, fmt, rnd) of the Float32 y."""
+    head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
+    rows, cols = x.shape
+    blocks = -(-cols // BLOCK)
+    width = blocks * BLOCK * (FORMAT_BITS[fmt] if 0 <= fmt < 6 else 8) // 8
+    elems = torch.empty((rows, width), dtype=torch.uint8, device=x.device) if elems_out is None else _flat(elems_out, "elems_out", (rows, width), torch.uint8, x.device)
+    scales = torch.empty((rows, blocks), dtype=torch.uint8, device=x.device) if scales_out is None else _flat(scales_out, "scales_out", (rows, blocks), torch.uint8, x.device)
+    with _On(x.device, stream) as st:
+        _check(lib().mx_rmsnorm_q(*head, fmt, rnd, elems.data_ptr(), scales.data_ptr(), *tail, st))
+    return elems, scales
+
+
+def mx_rmsnorm_b128(x, weight, eps, fmt, residual=None, h_out=None, y_out=None, rstd_out=None, elems_out=None, scales_out=None, stream=None):
+    """The norm delivered in 8 bits with a Float32 scale per 128: (elems, scales) as mx_quantize_b128(y, 1, fmt) of the Float32 y."""
+    head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
+    shape_e, shape_s = _b128_shapes(x.shape[0], x.shape[1], 1, False)
+    elems = torch.empty(shape_e, dtype=torch.uint8, device=x.device) if elems_out is None else _flat(elems_out, "elems_out", shape_e, torch.uint8, x.device)
+    scales = torch.empty(shape_s, dtype=torch.float32, device=x.device) if scales_out is None else _flat(scales_out, "scales_out", shape_s, torch.float32, x.device)
+    with _On(x.device, stream) as st:
+        _check(lib().mx_rmsnorm_b128(*head, fmt, elems.data_ptr(), scales.data_ptr(), *tail, st))
+    return elems, scales
+
+
+def mx_rmsnorm_bwd(dy, h, weight, rstd, dh=None, dx_out=None, want_dweight=True, stream=None):
+    """Gradients of the norm: (dx, dweight float32 [cols], or None with want_dweight=False).  h and rstd as the forward pass left them; dh, the gradient that
+    reaches h by other ways, is added to dx.  dx_out may be dy, h or dh."""
+    ldy = _rows(dy, "dy")
+    rows, cols = dy.shape
+    ldh = _rows(h, "h", dy)
+    lddh = _rows(dh, "dh", dy) if dh is not None else 0
+    w_dt = DT_F32
+    if weight is not None:
+        _flat(weight, "weight", (cols,), weight.dtype, dy.device)
+        w_dt = _dt(weight)
+    _flat(rstd, "rstd", (rows,), torch.float32, dy.device)
+    dx = _empty_rows(rows, cols, dy.dtype, dy.device) if dx_out is None else dx_out
+    lddx = _rows(dx, "dx_out", dy)
+    dweight = torch.empty((cols,), dtype=torch.float32, device=dy.device) if want_dweight else None
+    with _On(dy.device, stream) as st:
+        ws = _bwd_workspace(rows, cols, dy.device, stream) if want_dweight else None
+        wp, wb = _ws_args(ws)
+        _check(lib().mx_rmsnorm_bwd_ws(dy.data_ptr(), ldy, h.data_ptr(), ldh, None if weight is None else weight.data_ptr(), w_dt, rstd.data_ptr(),
+                                       None if dh is None else dh.data_ptr(), lddh, _dt(dy), rows, cols, dx.data_ptr(), lddx,
+                                       None if dweight is None else dweight.data_ptr(), wp, wb, st))
+    return dx, dweight
+
+
+def _bwd_workspace(rows, cols, device, stream):
+    """The partial sums' scratch memory from torch's caching allocator, or None for the library's own: as for the products, on torch's current
+    stream only, and not while it is captured."""
+    current = torch.cuda.current_stream()
+    if (stream is not None and stream.cuda_stream != current.cuda_stream) or torch.cuda.is_current_stream_capturing():
+        return None
+    need = lib().mx_rmsnorm_bwd_workspace_bytes(rows, cols)
+    try:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    except torch.cuda.OutOfMemoryError:
+        return None

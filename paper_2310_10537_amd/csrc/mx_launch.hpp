@@ -116,6 +116,25 @@ hipError_t launch_gemm_tiled_mx(int64_t M, int64_t N, int64_t K, const uint8_t *
                                 const uint8_t *Be, const uint8_t *Bs, int fmtB, uint8_t *Ce, uint8_t *Cs, int fmtC, int rndC,
                                 hipStream_t st);
 
+// 8-bit formats with a Float32 scale for each block of 128 along the lines, or each 128 x 128 tile; hipErrorNotSupported beyond 2^31 - 8 tiles,
+// or lines of more than about 2^33 elements
+hipError_t launch_cast_b128(const void *src, int src_dt, int64_t rows, int64_t cols, int64_t ld, int axis, bool tile, int fmt, uint8_t *elems,
+                            float *scales, hipStream_t st);
+hipError_t launch_dequant_b128(const uint8_t *elems, const float *scales, int fmt, int64_t rows, int64_t cols, int axis, bool tile, void *dst,
+                               int dst_dt, int64_t ld, hipStream_t st);
+
+// C = A B^T on such operands, K a multiple of 128
+hipError_t launch_gemm_b128(int64_t M, int64_t N, int64_t K, const uint8_t *Ae, const float *As, bool tileA, int fmtA, const uint8_t *Be,
+                            const float *Bs, bool tileB, int fmtB, void *C, int c_dt, int64_t ldc, hipStream_t st);
+
+// RMS norm (mx_norm.hpp: NormArgs, the output forms) and its gradients; the latter take norm_bwd_workspace bytes of scratch memory where dweight is wanted
+struct NormArgs;
+hipError_t launch_norm_f32(const NormArgs &a, int out, hipStream_t st);
+hipError_t launch_norm_bf16(const NormArgs &a, int out, hipStream_t st);
+size_t norm_bwd_workspace(int64_t rows, int64_t cols);
+hipError_t launch_norm_bwd(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *weight, int w_dt, const float *rstd, const void *dh,
+                           int64_t lddh, int dt, int64_t rows, int64_t cols, void *dx, int64_t lddx, float *dweight, hipStream_t st);
+
 // mx_gemm followed by the axis-1 cast of its Float32 result, fused where the tiled kernel applies
 hipError_t launch_gemm_q(int64_t M, int64_t N, int64_t K, const uint8_t *Ae, const uint8_t *As, int fmtA, const uint8_t *Be,
                          const uint8_t *Bs, int fmtB, uint8_t *Ce, uint8_t *Cs, int fmtC, int rndC, hipStream_t st);

@@ -1,0 +1,305 @@
+// Gradients of the RMS norm y = h rstd w (the cast behind it passes its gradient through), with g = dy w and xhat = h rstd:
+//     dx = rstd (g - xhat mean(g xhat)) + dh,        dweight = sum over rows of dy xhat.
+// dx is the gradient of x and of the residual alike; dh is the gradient that reaches h past the layer.
+// Bound by memory: dy, h (and dh) read and dx written, once; everything else is small.
+//
+// norm_bwd_kernel: a fixed number of work-groups walks the rows; a row lies in the registers of NT threads (a wave, or the
+// work-group) as packed pairs, the weight is kept unpacked from row to row, and every thread adds up its own columns'
+// part of dweight in Float32.  Each work-group writes one line of partial sums to scratch memory and
+// norm_bwd_weight_kernel adds the lines in a fixed order: no atomics, the same bits every time.
+// norm_bwd_long_kernel and norm_bwd_long_weight_kernel: rows that do not fit in registers; dy and h are read three times.
+#include "mx_norm.hpp"
+
+namespace mx {
+
+struct NormBwdArgs {
+    const void *dy, *h, *weight, *dh;
+    const float *rstd;
+    void *dx;
+    float *partial;       // [lines][cols], or nullptr: no dweight
+    int64_t rows, cols, lddy, ldh, lddh, lddx;
+    int w_dt;
+};
+
+template <int DT> struct Vec8 { uint32_t d[DT == DT_BF16 ? 4 : 8]; };
+
+// eight elements as they lie in memory (n of them; the rest zero), and one of them as Float32
+template <int DT>
+__device__ __forceinline__ Vec8<DT> fetch8(const void *p, int64_t at, int n)
+{
+    Vec8<DT> v;
+    if constexpr (DT == DT_BF16) {
+        const uint16_t *q = static_cast<const uint16_t *>(p) + at;
+        if (n >= 8) {
+            const uint4 t = ld16_nt(q);
+            v.d[0] = t.x; v.d[1] = t.y; v.d[2] = t.z; v.d[3] = t.w;
+        } else {
+            uint32_t e[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) e[i] = i < n ? q[i] : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; i++) v.d[i] = e[2 * i] | (e[2 * i + 1] << 16);
+        }
+    } else {
+        const uint32_t *q = static_cast<const uint32_t *>(p) + at;
+        if (n >= 8) {
+            const uint4 a = ld16_nt(q), b = ld16_nt(q + 4);
+            v.d[0] = a.x; v.d[1] = a.y; v.d[2] = a.z; v.d[3] = a.w;
+            v.d[4] = b.x; v.d[5] = b.y; v.d[6] = b.z; v.d[7] = b.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) v.d[i] = i < n ? q[i] : 0u;
+        }
+    }
+    return v;
+}
+template <int DT>
+__device__ __forceinline__ float elem(const Vec8<DT> &v, int i)
+{
+    if constexpr (DT == DT_BF16) return __uint_as_float(i & 1 ? v.d[i >> 1] & 0xFFFF0000u : v.d[i >> 1] << 16);
+    else return __uint_as_float(v.d[i]);
+}
+
+__device__ __forceinline__ void load_weight(const NormBwdArgs &a, int64_t col, int n, float (&w)[8])
+{
+    if (!a.weight) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i] = 1.0f;
+    } else if (a.w_dt == DT_BF16) {
+        load8<DT_BF16, false>(a.weight, col, n, w);
+    } else {
+        load8<DT_F32, false>(a.weight, col, n, w);
+    }
+}
+
+template <int DT, int NT, int VPT>
+__global__ __launch_bounds__(256) void norm_bwd_kernel(NormBwdArgs a)
+{
+    constexpr int RPW = 256 / NT;
+    __shared__ float lds[NT == 64 ? 256 * 8 : 2 * (NT / 64)];
+    const int t = threadIdx.x & (NT - 1);
+    float w[VPT][8], dw[VPT][8];
+#pragma unroll
+    for (int k = 0; k < VPT; k++) {
+        const int64_t col = (int64_t)(k * NT + t) * 8;
+        load_weight(a, col, inside(a.cols - col, 8), w[k]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) dw[k][i] = 0.0f;
+    }
+    const float inv = 1.0f / (float)a.cols;
+    int trip = 0;
+    for (int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / NT; row < a.rows; row += (int64_t)gridDim.x * RPW, trip ^= 1) {
+        Vec8<DT> dy[VPT], h[VPT], dh[VPT];
+#pragma unroll
+        for (int k = 0; k < VPT; k++) {
+            const int64_t col = (int64_t)(k * NT + t) * 8;
+            const int n = inside(a.cols - col, 8);
+            dy[k] = fetch8<DT>(a.dy, row * a.lddy + col, n);
+            h[k] = fetch8<DT>(a.h, row * a.ldh + col, n);
+        }
+        const float rstd = a.rstd[row];
+        if (a.dh) {
+#pragma unroll
+            for (int k = 0; k < VPT; k++) {
+                const int64_t col = (int64_t)(k * NT + t) * 8;
+                dh[k] = fetch8<DT>(a.dh, row * a.lddh + col, inside(a.cols - col, 8));
+            }
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < VPT; k++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float d = elem<DT>(dy[k], i), x = elem<DT>(h[k], i) * rstd;
+                sum = fmaf(d * w[k][i], x, sum);
+                dw[k][i] = fmaf(d, x, dw[k][i]);
+            }
+        // (two places in LDS taken in turn: a barrier in between keeps a fast wave from writing where a slow one still reads)
+        const float mean = row_sum<NT>(sum, lds + (NT == 64 ? 0 : trip * (NT / 64))) * inv;
+#pragma unroll
+        for (int k = 0; k < VPT; k++) {
+            const int64_t col = (int64_t)(k * NT + t) * 8;
+            const int n = inside(a.cols - col, 8);
+            float dx[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float g = elem<DT>(dy[k], i) * w[k][i], x = elem<DT>(h[k], i) * rstd;
+                dx[i] = rstd * fmaf(-x, mean, g);
+            }
+            if (a.dh) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) dx[i] += elem<DT>(dh[k], i);
+            }
+            if (n > 0) put8<DT>(a.dx, row * a.lddx + col, n, dx);
+        }
+    }
+    if (!a.partial) return;
+    float *line = a.partial + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+    for (int k = 0; k < VPT; k++) {
+        const int64_t col = (int64_t)(k * NT + t) * 8;
+        const int n = inside(a.cols - col, 8);
+        if constexpr (NT == 64) {                     // four rows at a time: their waves' sums in order
+            if (k > 0) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; i++) lds[threadIdx.x * 8 + i] = dw[k][i];
+            __syncthreads();
+            if (threadIdx.x < 64) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float v = ((lds[t * 8 + i] + lds[(64 + t) * 8 + i]) + lds[(128 + t) * 8 + i]) + lds[(192 + t) * 8 + i];
+                    if (i < n) line[col + i] = v;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (i < n) line[col + i] = dw[k][i];
+        }
+    }
+}
+
+// dweight[c] = partial[0][c] + partial[1][c] + ..., 16 columns and 16 runs of lines a work-group
+__global__ __launch_bounds__(256) void norm_bwd_weight_kernel(const float *__restrict__ partial, int lines, int64_t cols, float *__restrict__ dweight)
+{
+    __shared__ float part[16][17];
+    const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int64_t col = (int64_t)blockIdx.x * 16 + c;
+    float sum = 0.0f;
+    if (col < cols) {
+        int l = g;
+        for (; l + 112 < lines; l += 128) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[j] = partial[(int64_t)(l + 16 * j) * cols + col];
+#pragma unroll
+            for (int j = 0; j < 8; j++) sum += v[j];
+        }
+        for (; l < lines; l += 16) sum += partial[(int64_t)l * cols + col];
+    }
+    part[g][c] = sum;
+    __syncthreads();
+    if (g == 0 && col < cols) {
+        for (int j = 1; j < 16; j++) sum += part[j][c];
+        dweight[col] = sum;
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
+{
+    __shared__ float lds[4];
+    const int64_t row = blockIdx.x;
+    const float rstd = a.rstd[row];
+    float sum = 0.0f;
+    for (int64_t col = threadIdx.x * 8; col < a.cols; col += 2048) {
+        const int n = inside(a.cols - col, 8);
+        float w[8];
+        load_weight(a, col, n, w);
+        const Vec8<DT> dy = fetch8<DT>(a.dy, row * a.lddy + col, n), h = fetch8<DT>(a.h, row * a.ldh + col, n);
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum = fmaf(elem<DT>(dy, i) * w[i], elem<DT>(h, i) * rstd, sum);
+    }
+    const float mean = row_sum<256>(sum, lds) / (float)a.cols;
+    for (int64_t col = threadIdx.x * 8; col < a.cols; col += 2048) {
+        const int n = inside(a.cols - col, 8);
+        float w[8], dx[8];
+        load_weight(a, col, n, w);
+        const Vec8<DT> dy = fetch8<DT>(a.dy, row * a.lddy + col, n), h = fetch8<DT>(a.h, row * a.ldh + col, n);
+#pragma unroll
+        for (int i = 0; i < 8; i++) dx[i] = rstd * fmaf(-elem<DT>(h, i) * rstd, mean, elem<DT>(dy, i) * w[i]);
+        if (a.dh) {
+            const Vec8<DT> dh = fetch8<DT>(a.dh, row * a.lddh + col, n);
+#pragma unroll
+            for (int i = 0; i < 8; i++) dx[i] += elem<DT>(dh, i);
+        }
+        put8<DT>(a.dx, row * a.lddx + col, n, dx);
+    }
+}
+
+// partial sums of dweight over the rows of line blockIdx.y, 2048 columns a work-group
+template <int DT>
+__global__ __launch_bounds__(256) void norm_bwd_long_weight_kernel(NormBwdArgs a)
+{
+    const int64_t col = (int64_t)blockIdx.x * 2048 + threadIdx.x * 8;
+    const int n = inside(a.cols - col, 8);
+    if (n == 0) return;
+    float dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float rstd = a.rstd[row];
+        const Vec8<DT> dy = fetch8<DT>(a.dy, row * a.lddy + col, n), h = fetch8<DT>(a.h, row * a.ldh + col, n);
+#pragma unroll
+        for (int i = 0; i < 8; i++) dw[i] = fmaf(elem<DT>(dy, i), elem<DT>(h, i) * rstd, dw[i]);
+    }
+    float *line = a.partial + (int64_t)blockIdx.y * a.cols;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (i < n) line[col + i] = dw[i];
+}
+
+// Columns that fit in registers: 8192 for a work-group.
+constexpr int64_t NORM_BWD_COLS = 8192;
+
+// Lines of partial sums: as many work-groups as the chip holds two of per compute unit, fewer where there are fewer rows.
+int norm_bwd_lines(int64_t rows, int64_t cols)
+{
+    const int64_t need = cols > NORM_BWD_COLS ? rows : cols <= 2048 ? (rows + 3) / 4 : rows;
+    const int64_t most = cols > NORM_BWD_COLS ? 64 : 512;
+    return (int)(need < most ? need : most);
+}
+
+size_t norm_bwd_workspace(int64_t rows, int64_t cols)
+{
+    if (rows <= 0 || cols <= 0) return 0;
+    return ((size_t)norm_bwd_lines(rows, cols) * (size_t)cols * 4 + 255) & ~(size_t)255;
+}
+
+template <int DT>
+static hipError_t launch_norm_bwd_t(const NormBwdArgs &a, int lines, float *dweight, hipStream_t st)
+{
+    const dim3 b(256), g((unsigned)lines);
+    if (a.cols > NORM_BWD_COLS) {
+        if (a.rows > ((int64_t)1 << 31) - 1 || a.cols > ((int64_t)1 << 36)) return hipErrorNotSupported;
+        if (a.partial)                                // first: dx may take the place of dy
+            hipLaunchKernelGGL((norm_bwd_long_weight_kernel<DT>), dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)lines), b, 0, st, a);
+        hipLaunchKernelGGL((norm_bwd_long_kernel<DT>), dim3((unsigned)a.rows), b, 0, st, a);
+    } else if (a.cols <= 512) {
+        hipLaunchKernelGGL((norm_bwd_kernel<DT, 64, 1>), g, b, 0, st, a);
+    } else if (a.cols <= 1024) {
+        hipLaunchKernelGGL((norm_bwd_kernel<DT, 64, 2>), g, b, 0, st, a);
+    } else if (a.cols <= 2048) {
+        hipLaunchKernelGGL((norm_bwd_kernel<DT, 64, 4>), g, b, 0, st, a);
+    } else if (a.cols <= 4096) {
+        hipLaunchKernelGGL((norm_bwd_kernel<DT, 256, 2>), g, b, 0, st, a);
+    } else {
+        hipLaunchKernelGGL((norm_bwd_kernel<DT, 256, 4>), g, b, 0, st, a);
+    }
+    if (a.partial)
+        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((a.cols + 15) / 16)), b, 0, st, a.partial, lines, a.cols, dweight);
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_bwd(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *weight, int w_dt, const float *rstd, const void *dh, int64_t lddh,
+                           int dt, int64_t rows, int64_t cols, void *dx, int64_t lddx, float *dweight, hipStream_t st)
+{
+    NormBwdArgs a = {dy, h, weight, dh, rstd, dx, nullptr, rows, cols, lddy, ldh, lddh, lddx, w_dt};
+    if (rows == 0) {                                  // an empty sum
+        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(256), 0, st, a.partial, 0, cols, dweight);
+        return hipGetLastError();
+    }
+    uint8_t *ws = nullptr;
+    if (dweight) {
+        const hipError_t e = ws_acquire(norm_bwd_workspace(rows, cols), st, &ws);
+        if (e != hipSuccess) return e;
+        a.partial = reinterpret_cast<float *>(ws);
+    }
+    const int lines = norm_bwd_lines(rows, cols);
+    hipError_t e = dt == DT_BF16 ? launch_norm_bwd_t<DT_BF16>(a, lines, dweight, st) : launch_norm_bwd_t<DT_F32>(a, lines, dweight, st);
+    if (ws) {
+        const hipError_t r = ws_release(ws, st);
+        if (e == hipSuccess) e = r;
+    }
+    return e;
+}
+
+}  // namespace mx

@@ -1,0 +1,130 @@
+// RMS norm with the residual's addition and a cast of the result:
+//     h = x + residual rounded to the tensors' type,  rstd = 1 / sqrt(mean(h^2) + eps),  y = (h w) rstd,
+// delivered as any of: h, y in the tensors' type, rstd, and the cast of the Float32 y to an MX format or to 8 bits with a
+// Float32 scale per 128.  (h w first: for bf16 h and w that product is exact, so y carries one rounding and that of rstd.)
+// Bound by memory: x and the residual read, h and the codes written, all once.
+//
+// norm_kernel: a row stays in the registers of NT threads, VPT vectors of eight elements each, between the sum of squares and the output; NT = 64: a wave a
+// row and no barrier, four rows a work-group; NT = 256: the work-group a row.  norm_long_kernel: rows that do not fit; h is read
+// (or added up) a second time.
+#pragma once
+
+#include "mx_norm.hpp"
+
+namespace mx {
+
+template <int OUT>
+__device__ __forceinline__ void norm_modes()
+{
+    if constexpr (OUT == FP8_E4M3 || OUT == FP8_E5M2 || OUT == OUT_B128_E4M3 || OUT == OUT_B128_E5M2) fp8_saturate_mode();
+}
+
+template <int DT>
+__device__ __forceinline__ void load_sum(const NormArgs &a, int64_t row, int64_t col, int n, float (&h)[8])
+{
+    load8<DT>(a.x, row * a.ldx + col, n, h);
+    if (a.residual) {
+        float r[8];
+        load8<DT>(a.residual, row * a.ldr + col, n, r);
+#pragma unroll
+        for (int i = 0; i < 8; i++) h[i] = held<DT>(h[i] + r[i]);
+    }
+}
+
+template <int OUT, int DT>
+__device__ __forceinline__ void put_vector(const NormArgs &a, int64_t row, int vec, bool on, const float (&h)[8], float rstd)
+{
+    const int64_t col = (int64_t)vec * 8;
+    const int n = on ? inside(a.cols - col, 8) : 0;
+    float y[8], w[8];
+    if (a.weight) {
+        if (a.w_dt == DT_BF16) load8<DT_BF16, false>(a.weight, col, n, w);
+        else load8<DT_F32, false>(a.weight, col, n, w);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) y[i] = i < n ? (a.weight ? h[i] * w[i] : h[i]) * rstd : 0.0f;    // (a NaN or infinite rstd stays out of the fill)
+    if (a.y && n > 0) put8<DT>(a.y, row * a.ldy + col, n, y);
+    put_cast<OUT>(y, a.rnd, a.elems, a.scales, row, vec, a.nvec, on);
+}
+
+template <int OUT, int DT, int NT, int VPT>
+__global__ __launch_bounds__(256) void norm_kernel(NormArgs a)
+{
+    norm_modes<OUT>();
+    __shared__ float lds[NT / 64];
+    constexpr int RPW = 256 / NT;                     // rows a work-group
+    const int t = threadIdx.x & (NT - 1);
+    const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / NT;
+    if (NT == 64 && row >= a.rows) return;            // (a whole wave; the kernel has no barrier then)
+    float h[VPT][8], sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < VPT; k++) {
+        const int64_t col = (int64_t)(k * NT + t) * 8;
+        load_sum<DT>(a, row, col, inside(a.cols - col, 8), h[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < VPT; k++) {
+        const int64_t col = (int64_t)(k * NT + t) * 8;
+        const int n = inside(a.cols - col, 8);
+        if (a.h && n > 0) put8<DT>(a.h, row * a.ldh + col, n, h[k]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum = fmaf(h[k][i], h[k][i], sum);
+    }
+    const float rstd = rsqrtf(row_sum<NT>(sum, lds) / (float)a.cols + a.eps);
+    if (a.rstd && t == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int k = 0; k < VPT; k++) put_vector<OUT, DT>(a, row, k * NT + t, k * NT + t < a.nvec, h[k], rstd);
+}
+
+template <int OUT, int DT>
+__global__ __launch_bounds__(256) void norm_long_kernel(NormArgs a)
+{
+    norm_modes<OUT>();
+    __shared__ float lds[4];
+    const int64_t row = blockIdx.x;
+    float sum = 0.0f;
+    for (int vec = threadIdx.x; vec < a.nvec; vec += 256) {
+        const int64_t col = (int64_t)vec * 8;
+        const int n = inside(a.cols - col, 8);
+        float h[8];
+        load_sum<DT>(a, row, col, n, h);
+        if (a.h && n > 0) put8<DT>(a.h, row * a.ldh + col, n, h);
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum = fmaf(h[i], h[i], sum);
+    }
+    const float rstd = rsqrtf(row_sum<256>(sum, lds) / (float)a.cols + a.eps);
+    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+    const int trips = (a.nvec + 255) / 256;           // (the same number for every lane: they share blocks)
+    for (int k = 0; k < trips; k++) {
+        const int vec = k * 256 + threadIdx.x;
+        const bool on = vec < a.nvec;
+        const int64_t col = (int64_t)vec * 8;
+        const int n = on ? inside(a.cols - col, 8) : 0;
+        float h[8];
+        // h may have been written over x or the residual: then it is read where it was written (by this very thread)
+        if (a.h) load8<DT, false>(a.h, row * a.ldh + col, n, h);
+        else load_sum<DT>(a, row, col, n, h);
+        put_vector<OUT, DT>(a, row, vec, on, h, rstd);
+    }
+}
+
+// Which form: a wave a row up to 4096 columns where there are rows enough to fill the chip with waves, else the work-group.
+template <int OUT, int DT>
+static hipError_t launch_norm_t(const NormArgs &a, hipStream_t st)
+{
+    const int64_t most = ((int64_t)1 << 31) - 1;
+    const bool waves = a.nvec <= 512 && a.rows >= 1024;
+    const int64_t grid = waves ? (a.rows + 3) / 4 : a.rows;
+    if (grid > most) return hipErrorNotSupported;
+    const dim3 g((unsigned)grid), b(256);
+    if (waves && a.nvec <= 128) hipLaunchKernelGGL((norm_kernel<OUT, DT, 64, 2>), g, b, 0, st, a);
+    else if (waves && a.nvec <= 256) hipLaunchKernelGGL((norm_kernel<OUT, DT, 64, 4>), g, b, 0, st, a);
+    else if (waves) hipLaunchKernelGGL((norm_kernel<OUT, DT, 64, 8>), g, b, 0, st, a);
+    else if (a.nvec <= 512) hipLaunchKernelGGL((norm_kernel<OUT, DT, 256, 2>), g, b, 0, st, a);
+    else if (a.nvec <= 1024) hipLaunchKernelGGL((norm_kernel<OUT, DT, 256, 4>), g, b, 0, st, a);
+    else if (a.nvec <= 2048) hipLaunchKernelGGL((norm_kernel<OUT, DT, 256, 8>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((norm_long_kernel<OUT, DT>), g, b, 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace mx
