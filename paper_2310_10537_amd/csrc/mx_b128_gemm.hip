@@ -1,5 +1,6 @@
 // Dispatch of the products with a scale per 128 (kernels in mx_b128_gemm.hpp, mx_b128_gemm_few.hpp).
 #include "mx_b128_gemm_few.hpp"
+#include "mx_b128_gemm_tile.hpp"
 
 namespace mx {
 
@@ -8,8 +9,8 @@ static hipError_t launch_tiles(const Gemm128 &g, hipStream_t st)
 {
     const int64_t tm = (g.M + 16 * MB * WM - 1) / (16 * MB * WM), tn = (g.N + 16 * NB * WN - 1) / (16 * NB * WN);
     if (tm > ((int64_t)1 << 30) / tn) return hipErrorNotSupported;
-    const Raster rast = choose_raster((int)tm, (int)tn, 8, 8);
-    hipLaunchKernelGGL((gemm128_kernel<FA, FB, CDT, ROWS_B, MB, NB, WM, WN>), dim3(raster_grid(rast, (int)tm, (int)tn)), dim3(64 * WM * WN), 0, st, g, (int)tm, (int)tn, rast);
+    const Bands order = bands(tm, tn, 6);
+    hipLaunchKernelGGL((gemm128_kernel<FA, FB, CDT, ROWS_B, MB, NB, WM, WN>), dim3(8 * order.per_xcd), dim3(64 * WM * WN), 0, st, g, order);
     return hipGetLastError();
 }
 
@@ -28,10 +29,11 @@ static hipError_t launch_rows(const Gemm128 &g, hipStream_t st)
     if (g.M <= 16) return launch_few<FA, FB, CDT, ROWS_B, 1, 1, 4>(g, st);
     if (g.M <= 32) return launch_few<FA, FB, CDT, ROWS_B, 2, 1, 2>(g, st);
     if (g.M <= 64) return launch_few<FA, FB, CDT, ROWS_B, 4, 1, 2>(g, st);
-    const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256), mid = ((g.M + 127) / 128) * ((g.N + 127) / 128);
-    if (large >= 256) return launch_tiles<FA, FB, CDT, ROWS_B, 4, 8, 4, 2>(g, st);
-    if (mid >= 256) return launch_tiles<FA, FB, CDT, ROWS_B, 4, 4, 2, 2>(g, st);
-    return launch_tiles<FA, FB, CDT, ROWS_B, 2, 2, 2, 2>(g, st);
+    const int64_t large = ((g.M + 255) / 256) * ((g.N + 255) / 256);
+    const int64_t T = g.K / 128;
+    if (large >= 200 && T >= TILE_MIN_BLOCKS && T < 1 << 17) return launch_tile<FA, FB, CDT, ROWS_B, 4, 8, 4, 2, 1>(g, st);
+    if (T >= 2 * TILE_MIN_BLOCKS && T % 2 == 0 && T < 1 << 17) return launch_tile<FA, FB, CDT, ROWS_B, 4, 4, 2, 2, 2>(g, st);
+    return launch_tiles<FA, FB, CDT, ROWS_B, 4, 4, 2, 2>(g, st);
 }
 
 template <int FA, int FB>

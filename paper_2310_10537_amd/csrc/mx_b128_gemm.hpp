@@ -14,7 +14,6 @@
 
 #include "mx_b128.hpp"
 #include "mx_gemm_frag.hpp"
-#include "mx_gemm_raster.hpp"
 #include "mx_launch.hpp"
 
 namespace mx {
@@ -31,6 +30,26 @@ struct Gemm128 {
     int64_t ldc;
 };
 
+// Order of the tiles of C, for a grid of any size.  Work-groups are dealt round-robin to the 8 XCDs, each with its own L2, and the 32 or 64 that an XCD
+// works on at a time walk K in step: what they fetch per step is a slab of A for each of their tile rows and one of B for each tile
+// column.  So the tiles are numbered in bands of h rows, column by column, and each XCD takes an eighth of the numbers: its running tiles
+// form a patch of h rows.
+struct Bands { int tiles_m, tiles_n, h, per_xcd; };
+inline Bands bands(int64_t tiles_m, int64_t tiles_n, int h)
+{
+    return Bands{(int)tiles_m, (int)tiles_n, (int)(tiles_m < h ? tiles_m : h), (int)((tiles_m * tiles_n + 7) / 8)};
+}
+// tile of work-group b; false when it has none
+__device__ __forceinline__ bool band_tile(const Bands &r, int b, int &tm, int &tn)
+{
+    const int at = (b & 7) * r.per_xcd + (b >> 3), area = r.h * r.tiles_n;
+    if (at >= r.tiles_m * r.tiles_n) return false;
+    const int band = at / area, in = at - band * area, left = r.tiles_m - band * r.h, h = left < r.h ? left : r.h;
+    tn = in / h;
+    tm = band * r.h + in - tn * h;
+    return true;
+}
+
 // 128 products of each of 16 x 16 entries, from zero (unit scales: plain products)
 template <int FA, int FB>
 __device__ __forceinline__ v4f_t block_product(const v8i_t &b, const v8i_t &a)
@@ -39,38 +58,77 @@ __device__ __forceinline__ v4f_t block_product(const v8i_t &b, const v8i_t &a)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, v4f_t{0.f, 0.f, 0.f, 0.f}, HB, HA, 0, 0, 0, 0);
 }
 
-// Four consecutive columns of a row, as far as they lie inside C.  vec: columns and pitch allow one store
+// N consecutive values of a row of C to it, as far as they lie inside (left: columns that do).  Rows start anywhere: the vector stores assume the
+// alignment of an element only.
+typedef float f32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void store4_f32(float *o, int64_t left, const v4f_t &v)
+{
+    if (left >= 4) {
+        *reinterpret_cast<f32x4_at4 *>(o) = f32x4_at4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; i++)
+            if (i < left) o[i] = v[i];
+    }
+}
+template <int ND>
+__device__ __forceinline__ void store_bf16(uint16_t *o, int64_t left, const uint32_t (&d)[ND])
+{
+    if (left >= 2 * ND) {
+        if constexpr (ND == 4) *reinterpret_cast<u32x4_at2 *>(o) = u32x4_at2{d[0], d[1], d[2], d[3]};
+        else *reinterpret_cast<u32x2_at2 *>(o) = u32x2_at2{d[0], d[1]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2 * ND - 1; i++)
+            if (i < left) o[i] = (uint16_t)(d[i >> 1] >> (16 * (i & 1)));
+    }
+}
+// one instruction tile's four columns of a lane's row
 template <int CDT>
-__device__ __forceinline__ void store4(void *__restrict__ C, int64_t at, int n, bool vec, const v4f_t &v)
+__device__ __forceinline__ void store4(void *__restrict__ C, int64_t at, int64_t left, const v4f_t &v)
 {
     if constexpr (CDT == DT_F32) {
-        float *o = static_cast<float *>(C) + at;
-        if (n >= 4 && vec) {
-            *reinterpret_cast<float4 *>(o) = make_float4(v[0], v[1], v[2], v[3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (i < n) o[i] = v[i];
-        }
+        store4_f32(static_cast<float *>(C) + at, left, v);
     } else {
-        uint16_t *o = static_cast<uint16_t *>(C) + at;
-        const uint32_t p0 = pack_bf16(v[0], v[1]), p1 = pack_bf16(v[2], v[3]);
-        if (n >= 4 && vec) {
-            *reinterpret_cast<uint2 *>(o) = make_uint2(p0, p1);
+        const uint32_t d[2] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        store_bf16<2>(static_cast<uint16_t *>(C) + at, left, d);
+    }
+}
+// A wave's MX x NY instruction tiles, rows from row0 and columns from col0 on.  bf16: the lanes q and q ^ 1 of a row hold neighbouring column
+// groups; they trade between two tiles (the row swap of the lane permutes does exactly that), so that each stores eight columns: 64
+// contiguous bytes a row and instruction.
+template <int CDT, int MX, int NY, int MROWS>
+__device__ __forceinline__ void store_rows(const Gemm128 &g, const v4f_t (&acc)[MROWS][NY], int64_t row0, int64_t col0, int i, int q)
+{
+#pragma unroll
+    for (int x = 0; x < MX; x++) {
+        const int64_t r = row0 + 16 * x + i;
+        if constexpr (CDT == DT_F32) {
+#pragma unroll
+            for (int y = 0; y < NY; y++) {
+                const int64_t c = col0 + 16 * y + 4 * q;
+                if (r < g.M && c < g.N) store4<CDT>(g.C, r * g.ldc + c, g.N - c, acc[x][y]);
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (i < n) o[i] = (uint16_t)((i & 2 ? p1 : p0) >> (16 * (i & 1)));
+            for (int y = 0; y < NY; y += 2) {
+                const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[x][y][0], acc[x][y][1]), pack_bf16(acc[x][y + 1][0], acc[x][y + 1][1]), false, false);
+                const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[x][y][2], acc[x][y][3]), pack_bf16(acc[x][y + 1][2], acc[x][y + 1][3]), false, false);
+                const uint32_t d[4] = {lo[0], hi[0], lo[1], hi[1]};
+                const int64_t c = col0 + 16 * y + 16 * (q & 1) + 4 * (q & 2);
+                if (r < g.M && c < g.N) store_bf16<4>(static_cast<uint16_t *>(g.C) + r * g.ldc + c, g.N - c, d);
+            }
         }
     }
 }
-
 // Work-group tile BM x BN: WM x WN waves of 16 MB x 16 NB entries.  K in steps of one block through two LDS buffers, laid out as in the MX
 // kernels (128 bytes a row, chunk c of row r in slot c ^ ((r >> 1) & 7): direct loads fill any permutation of 16-byte slots, and the
 // operand reads meet no bank twice).  Rows beyond M and columns beyond N read the last valid one and are not stored.
 // Scales travel four blocks at a time, 16 bytes a row, by way of registers into [block][row] in LDS.
 template <int FA, int FB, int CDT, bool ROWS_B, int MB, int NB, int WM, int WN>
-__global__ __launch_bounds__(64 * WM *WN, WM *WN >= 8 ? 2 : 1) void gemm128_kernel(Gemm128 g, int tiles_m, int tiles_n, Raster rast)
+__global__ __launch_bounds__(64 * WM * WN, 2) void gemm128_kernel(Gemm128 g, Bands order)
 {
     constexpr int NW = WM * WN, BM = 16 * MB * WM, BN = 16 * NB * WN, NTHREADS = 64 * NW;
     constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
@@ -83,7 +141,7 @@ __global__ __launch_bounds__(64 * WM *WN, WM *WN >= 8 ? 2 : 1) void gemm128_kern
     const int wm = wave / WN, wn = wave - wm * WN;
     const int i = lane & 15, q = lane >> 4;
     int tm, tn;
-    if (!raster_tile(rast, (int)blockIdx.x, tiles_m, tiles_n, tm, tn)) return;
+    if (!band_tile(order, (int)blockIdx.x, tm, tn)) return;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int T = (int)(g.K / 128);
 
@@ -222,18 +280,7 @@ __global__ __launch_bounds__(64 * WM *WN, WM *WN >= 8 ? 2 : 1) void gemm128_kern
         if (next_scales) park_scales(G + 1);
     }
 
-    const bool vec = (g.ldc & 3) == 0;
-#pragma unroll
-    for (int x = 0; x < MB; x++) {
-        const int64_t r = m0 + wm * 16 * MB + 16 * x + i;
-        if (r >= g.M) continue;
-#pragma unroll
-        for (int y = 0; y < NB; y++) {
-            const int64_t c = n0 + wn * 16 * NB + 16 * y + 4 * q, left = g.N - c;
-            const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-            if (n > 0) store4<CDT>(g.C, r * g.ldc + c, n, vec, acc[x][y]);
-        }
-    }
+    store_rows<CDT, MB, NB>(g, acc, m0 + wm * 16 * MB, n0 + wn * 16 * NB, i, q);
 }
 
 }  // namespace mx

@@ -99,8 +99,6 @@ __global__ __launch_bounds__(512) void gemm128_few_kernel(Gemm128 g)
             for (int y = 0; y < NB; y++) *reinterpret_cast<v4f_t *>(red[wave - 1][x * NB + y][lane]) = acc[x][y];
     }
     __syncthreads();
-    // tile k of the MB x NB is added up and stored by wave k
-    const bool vec = (g.ldc & 3) == 0;
 #pragma unroll
     for (int x = 0; x < MB; x++)
 #pragma unroll
@@ -113,9 +111,8 @@ __global__ __launch_bounds__(512) void gemm128_few_kernel(Gemm128 g)
 #pragma unroll
                 for (int e = 0; e < 4; e++) v[e] += o[e];
             }
-            const int64_t r = m0 + 16 * x + i, c = n0 + 16 * y + 4 * q, left = g.N - c;
-            const int n = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-            if (r < g.M && n > 0) store4<CDT>(g.C, r * g.ldc + c, n, vec, v);
+            const int64_t r = m0 + 16 * x + i, c = n0 + 16 * y + 4 * q;
+            if (r < g.M && c < g.N) store4<CDT>(g.C, r * g.ldc + c, g.N - c, v);
         }
 }
 
