@@ -74,9 +74,9 @@ int mx_dequantize_b128(const void *elems, const float *scales, mx_format_t fmt,
  * product (see mx_gemm); the block's sum is multiplied by the Float32 product of the
  * two scales and added in Float32.  A product of scales has to be inside Float32's
  * range: where it overflows, an entry is infinite or NaN; below 2^-126 it loses bits.
- * Up to 64 rows eight waves share K and their sums are added in a fixed order; else
- * an entry's blocks are added in the order of K.  Which of the two depends on the
- * shape alone: results are reproducible.
+ * The blocks of an entry are added in the order of K, or in the order of K within each
+ * half or eighth of K and these sums in order; which, depends on the shape alone:
+ * results are reproducible.
  * C, c_dt, ldc, alignment as mx_gemm (scales 16-byte aligned too).  rows of C beyond
  * M and columns beyond N are not touched.
  * MX_ERR_UNSUPPORTED: more than 2^30 tiles of C, or K of 2^38 and more.

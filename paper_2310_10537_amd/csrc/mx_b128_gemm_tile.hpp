@@ -1,8 +1,8 @@
 // Larger products with a scale per 128 (the formula and the operand order: mx_b128_gemm.hpp).
 //
 // Eight waves, two on each SIMD, in KS groups of WM x WN that share the range of K; a wave owns 16 MB x 16 NB entries, a group 16 MB WM x
-// 16 NB WN.  Two forms are used: 256 x 256 (one group of 4 x 2 waves, 64 x 128 entries each) and 128 x 128 (two groups of 2 x 2 waves, 64 x 64
-// entries each, half of K each: as many waves a tile where there are few tiles).
+// 16 NB WN.  Three forms are used: 256 x 256 and 256 x 128 (one group of 4 x 2 waves, 64 x 128 or 64 x 64 entries each) and 128 x 128 (two groups
+// of 2 x 2 waves, 64 x 64 entries each, half of K each: as many waves a tile where there are few tiles).
 // The scaling of the partial sums is vector work, 4 instructions of 4 clocks beside each matrix instruction of 32, and a wave issues an
 // instruction about every 5 clocks, so one wave on a SIMD cannot issue all that a matrix instruction wants beside it (four waves of 96 x 128 entries, operands in
 // accumulation registers: 383 us for 8192 x 11008 x 4096, 351 for 2048 x 8192 x 16384 with a scale a column; eight waves: 374 and 275).  With two, one

@@ -102,16 +102,17 @@ def test_largest_and_smallest_magnitudes(mx):
 # ---------------------------------------------------------------------------------------------
 def integer_operand(rows, K, fmt, tile, g):
     """Codes of whole numbers -4 .. 4 and power-of-two scales: every sum of the product is exact in Float32 in any order."""
-    codes = {abs(v): int(np.flatnonzero(model.table(fmt)[:124] == abs(v))[0]) for v in range(5)}
-    v = g.integers(-4, 5, (rows, K))
-    e = np.vectorize(codes.get)(np.abs(v)).astype(np.uint8) | np.where(v < 0, 128, 0).astype(np.uint8)
+    codes = np.array([np.flatnonzero(model.table(fmt)[:124] == v)[0] for v in range(5)], dtype=np.uint8)
+    v = g.integers(-4, 5, (rows, K), dtype=np.int8)
+    e = codes[np.abs(v)] | np.where(v < 0, 128, 0).astype(np.uint8)
     shape = (-(-rows // 128) if tile else rows, K // 128)
     s = (2.0 ** g.integers(-2, 3, shape)).astype(np.float32)
     return e, s
 
 
 GEMMS = [(1, 1, 128), (1, 200, 384), (2, 33, 1152), (15, 130, 1024), (16, 16, 2176), (17, 31, 640), (33, 129, 1280), (64, 300, 256), (65, 64, 128),
-         (100, 257, 896), (128, 128, 512), (130, 70, 640), (300, 515, 384)]
+         (100, 257, 896), (128, 128, 512), (130, 70, 640), (300, 515, 384), (9, 16500, 256), (20, 8200, 384), (30, 8192, 1152), (64, 8200, 1024), (70, 130, 2048),
+         (65, 257, 512), (200, 33000, 640), (257, 129, 1408), (1030, 8200, 768)]
 
 
 def product_operands(rows_a, rows_b, K, fa, fb, tiles, seed):
@@ -125,7 +126,8 @@ def test_product_exactly(mx, fa, fb, tiles):
     """Where no sum rounds, every entry is exact whatever the kernel, and nothing beside C is written."""
     for M, N, K in GEMMS:
         (ea, sa), (eb, sb) = product_operands(M, N, K, fa, fb, tiles, M + N + K)
-        want = torch.from_numpy(model.values(ea, sa, fa, tiles[0]) @ model.values(eb, sb, fb, tiles[1]).T)
+        va, vb = (torch.from_numpy(model.values(*o, np.float32)).cuda() for o in ((ea, sa, fa, tiles[0]), (eb, sb, fb, tiles[1])))
+        want = (va.double() @ vb.double().T.contiguous()).cpu()
         a, b = (to_dev(ea), to_dev(sa)), (to_dev(eb), to_dev(sb))
         for dt in (torch.float32, torch.bfloat16):
             for pad in (0, 3, 8):
