@@ -15,35 +15,50 @@
 
 namespace mx {
 
-// N consecutive elements at src (n of them inside the row; the rest is zero) as Float32 bit patterns
-template <int DT, int N>
-__device__ __forceinline__ void load_elems(const void *__restrict__ src, int64_t at, int n, uint32_t (&v)[N])
+// The 16 bytes at element `at` of which n elements lie inside the row, as they lie in memory (the rest is zero).
+template <int DT>
+__device__ __forceinline__ uint4 load16(const void *__restrict__ src, int64_t at, int n)
 {
-    static_assert(DT == DT_BF16 ? N == 8 : N == 4, "one 16-byte load");
+    constexpr int EPL = DT == DT_BF16 ? 8 : 4, ES = DT == DT_BF16 ? 2 : 4;
+    const uint8_t *g = static_cast<const uint8_t *>(src) + at * ES;
+    if (n == EPL) return ld16_nt(g);
+    uint32_t h[EPL];
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] = 0;
+    for (int i = 0; i < EPL; i++) h[i] = i >= n ? 0u : DT == DT_BF16 ? (uint32_t)reinterpret_cast<const uint16_t *>(g)[i] : reinterpret_cast<const uint32_t *>(g)[i];
+    if constexpr (DT == DT_BF16) return make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
+    else return make_uint4(h[0], h[1], h[2], h[3]);
+}
+// ... as Float32 bit patterns
+template <int DT>
+__device__ __forceinline__ void widen(const uint4 &t, uint32_t (&v)[DT == DT_BF16 ? 8 : 4])
+{
+    const uint32_t d[4] = {t.x, t.y, t.z, t.w};
     if constexpr (DT == DT_BF16) {
-        const uint16_t *p = static_cast<const uint16_t *>(src) + at;
-        if (n >= 8) {
-            const uint4 t = ld16_nt(p);
-            const uint32_t d[4] = {t.x, t.y, t.z, t.w};
-            widen_bf16<4>(d, v);
-        } else if (n > 0) {
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (i < n) v[i] = (uint32_t)p[i] << 16;
-        }
+        widen_bf16<4>(d, v);
     } else {
-        const uint32_t *p = static_cast<const uint32_t *>(src) + at;
-        if (n >= 4) {
-            const uint4 t = ld16_nt(p);
-            v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
-        } else if (n > 0) {
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (i < n) v[i] = p[i];
+        for (int i = 0; i < 4; i++) v[i] = d[i];
+    }
+}
+// The largest magnitude in 16-byte pieces, as a Float32 bit pattern; bf16 stays packed (half of a 32-bit maximum's work)
+template <int DT, int N>
+__device__ __forceinline__ uint32_t pieces_max(const uint4 (&t)[N])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int p = 0; p < N; p++) {
+        const uint32_t d[4] = {t[p].x, t[p].y, t[p].z, t[p].w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if constexpr (DT == DT_BF16) {
+                m = pk_absmax(m, d[i]);
+            } else {
+                const uint32_t k = d[i] & 0x7FFFFFFFu;
+                m = m > k ? m : k;
+            }
         }
     }
+    return DT == DT_BF16 ? pk_hmax(m) << 16 : m;
 }
 
 constexpr int ROW128_CHUNKS = 4;
@@ -62,7 +77,7 @@ __global__ __launch_bounds__(256) void cast128_row_kernel(const void *__restrict
     constexpr int EPL = DT == DT_BF16 ? 8 : 4, LPB = BLOCK128 / EPL;
     fp8_saturate_mode();
     const uint32_t u0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * ROW128_CHUNKS) + (threadIdx.x & 63);
-    uint32_t v[ROW128_CHUNKS][EPL];
+    uint4 d[ROW128_CHUNKS];
 #pragma unroll
     for (int c = 0; c < ROW128_CHUNKS; c++) {
         const uint32_t u = u0 + c * 64;
@@ -74,13 +89,24 @@ __global__ __launch_bounds__(256) void cast128_row_kernel(const void *__restrict
             n = left >= EPL ? EPL : left > 0 ? (int)left : 0;
             at = (int64_t)r * geom.ld + col;
         }
-        load_elems<DT, EPL>(src, at, n, v[c]);
+        d[c] = load16<DT>(src, at, n);
     }
 #pragma unroll
     for (int c = 0; c < ROW128_CHUNKS; c++) {
         const uint32_t u = u0 + c * 64;
-        uint32_t out[EPL / 4];
-        const float f = b128_quantize<FMT, EPL>(v[c], [](uint32_t m) { return LPB == 16 ? row16_max(m) : row32_max(m); }, out);
+        auto group = [](uint32_t m) { return LPB == 16 ? row16_max(m) : row32_max(m); };
+        uint32_t v[EPL], out[EPL / 4];
+        widen<DT>(d[c], v);
+        const uint4 one[1] = {d[c]};
+        uint32_t amax = group(pieces_max<DT, 1>(one));
+        float f;
+        if (amax < 0x7F800000u) {
+            f = b128_factor<FMT>(amax);
+            b128_convert<FMT, EPL>(v, f, out);
+        } else {                                      // (every lane of the block)
+            f = b128_factor<FMT>(group(finite_max(v)));
+            b128_convert_any<FMT, EPL>(v, f, out);
+        }
         if (u < geom.n_units) {
             uint8_t *o = elems + (int64_t)u * EPL;
             if constexpr (EPL == 8) *reinterpret_cast<uint2 *>(o) = make_uint2(out[0], out[1]);
@@ -111,40 +137,54 @@ __global__ __launch_bounds__(256) void cast128_tile_kernel(const void *__restric
     const int lr = threadIdx.x / LPR, lc = threadIdx.x % LPR;
     const int64_t col = tc * BLOCK128 + lc * EPL, left = cols - col;
     const int n = left >= EPL ? EPL : left > 0 ? (int)left : 0;
-    uint32_t v[NP][EPL];
+    uint4 t[NP];
 #pragma unroll
     for (int p = 0; p < NP; p++) {
         const int64_t r = tr * BLOCK128 + p * RPP + lr;
-        load_elems<DT, EPL>(src, r * ld + col, r < rows ? n : 0, v[p]);
+        t[p] = load16<DT>(src, r * ld + col, r < rows ? n : 0);
     }
-    uint32_t m = 0;
-#pragma unroll
-    for (int p = 0; p < NP; p++) {
-        const uint32_t k = raw_max(v[p]);
-        m = m > k ? m : k;
-    }
-    m = group256_max(m, slot[0]);
+    uint32_t m = group256_max(pieces_max<DT, NP>(t), slot[0]);
     const bool finite = m < 0x7F800000u;
     if (!finite) {                                    // (the whole work-group)
         m = 0;
-#pragma unroll
+#pragma unroll 1
         for (int p = 0; p < NP; p++) {
-            const uint32_t k = finite_max(v[p]);
+            uint32_t v[EPL];
+            widen<DT>(t[0], v);
+            const uint32_t k = finite_max(v);
             m = m > k ? m : k;
+            const uint4 first = t[0];                 // (the pieces move along: none is indexed by the loop counter)
+#pragma unroll
+            for (int j = 0; j + 1 < NP; j++) t[j] = t[j + 1];
+            t[NP - 1] = first;
         }
         m = group256_max(m, slot[1]);
     }
     const float f = b128_factor<FMT>(m);
-#pragma unroll
-    for (int p = 0; p < NP; p++) {
+    auto put = [&](int p, const uint32_t (&out)[EPL / 4]) {
         const int64_t r = tr * BLOCK128 + p * RPP + lr;
-        uint32_t out[EPL / 4];
-        if (finite) b128_convert<FMT, EPL>(v[p], f, out);
-        else b128_convert_any<FMT, EPL>(v[p], f, out);
-        if (r < rows) {
-            uint8_t *o = elems + (r * n_cb + tc) * BLOCK128 + lc * EPL;
-            if constexpr (EPL == 8) *reinterpret_cast<uint2 *>(o) = make_uint2(out[0], out[1]);
-            else *reinterpret_cast<uint32_t *>(o) = out[0];
+        if (r >= rows) return;
+        uint8_t *o = elems + (r * n_cb + tc) * BLOCK128 + lc * EPL;
+        if constexpr (EPL == 8) *reinterpret_cast<uint2 *>(o) = make_uint2(out[0], out[1]);
+        else *reinterpret_cast<uint32_t *>(o) = out[0];
+    };
+    if (finite) {
+#pragma unroll
+        for (int p = 0; p < NP; p++) {
+            uint32_t v[EPL], out[EPL / 4];
+            widen<DT>(t[p], v);
+            b128_convert<FMT, EPL>(v, f, out);
+            put(p, out);
+        }
+    } else {
+#pragma unroll 1
+        for (int p = 0; p < NP; p++) {
+            uint32_t v[EPL], out[EPL / 4];
+            widen<DT>(t[0], v);
+            b128_convert_any<FMT, EPL>(v, f, out);
+            put(p, out);
+#pragma unroll
+            for (int j = 0; j + 1 < NP; j++) t[j] = t[j + 1];
         }
     }
     if (threadIdx.x == 0) scales[blockIdx.x] = 1.0f / f;
@@ -172,25 +212,7 @@ __global__ __launch_bounds__(256) void cast128_col_kernel(const void *__restrict
 #pragma unroll
         for (int p = 0; p < NP; p++) {
             const int64_t r = tr * BLOCK128 + p * RPP + lr;
-            t[p] = make_uint4(0, 0, 0, 0);
-            if (r < rows) {
-                const uint8_t *g = static_cast<const uint8_t *>(src) + (r * ld + col) * ES;
-                if (n == EPL) {
-                    t[p] = ld16_nt(g);
-                } else if (n > 0) {
-                    if constexpr (DT == DT_BF16) {
-                        uint32_t h[8];
-#pragma unroll
-                        for (int i = 0; i < 8; i++) h[i] = i < n ? reinterpret_cast<const uint16_t *>(g)[i] : 0u;
-                        t[p] = make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
-                    } else {
-                        uint32_t h[4];
-#pragma unroll
-                        for (int i = 0; i < 4; i++) h[i] = i < n ? reinterpret_cast<const uint32_t *>(g)[i] : 0u;
-                        t[p] = make_uint4(h[0], h[1], h[2], h[3]);
-                    }
-                }
-            }
+            t[p] = load16<DT>(src, r * ld + col, r < rows ? n : 0);
         }
 #pragma unroll
         for (int p = 0; p < NP; p++) {

@@ -78,17 +78,17 @@ __device__ __forceinline__ float wave_sum(float v)
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
-// The sum over the NT threads that share a row, in each of them.  NT = 64: a wave; else the work-group, by way of LDS (NT / 64 floats).
-template <int NT>
+// The sum over the threads that share a row, in each of them: a wave, or the work-group by way of LDS (a float for each of its waves).
+template <bool WAVE>
 __device__ __forceinline__ float row_sum(float v, float *lds)
 {
     v = wave_sum(v);
-    if constexpr (NT > 64) {
+    if constexpr (!WAVE) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
         __syncthreads();
         v = lds[0];
-#pragma unroll
-        for (int i = 1; i < NT / 64; i++) v += lds[i];
+        const int waves = (int)blockDim.x >> 6;
+        for (int i = 1; i < waves; i++) v += lds[i];
     }
     return v;
 }
@@ -145,20 +145,27 @@ __device__ __forceinline__ uint32_t mx_quantize8(const uint32_t (&v)[8], int rnd
         return s;
     }
     if (!Fmt<FMT>::elem_nan && s == SCALE_NAN) return s;
-    uint32_t c[8];
-    if (rnd == ROUND_TOWARD_ZERO) {
-#pragma unroll
-        for (int i = 0; i < 8; i++) c[i] = encode_elem<FMT, ROUND_TOWARD_ZERO>(v[i], s);
-    } else if (rnd == ROUND_HALF_AWAY) {
-#pragma unroll
-        for (int i = 0; i < 8; i++) c[i] = encode_elem<FMT, ROUND_HALF_AWAY>(v[i], s);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) c[i] = encode_elem<FMT, ROUND_RNE>(v[i], s);
-    }
+    // the exact encoder, one element a trip from registers that move along: little code, which counts where a kernel runs for a few microseconds
+    // (6 bits: the converts want a whole block in a lane, so this is the only path, and nearest-even is unrolled)
     uint64_t bits = 0;
+    if (w == 6 && rnd == ROUND_RNE) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) bits |= (uint64_t)c[i] << (w * i);
+        for (int i = 0; i < 8; i++) bits |= (uint64_t)encode_elem<FMT, ROUND_RNE>(v[i], s) << (w * i);
+        out[0] = (uint32_t)bits;
+        out[1] = (uint32_t)(bits >> 32);
+        return s;
+    }
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) r[i] = v[i];
+#pragma unroll 1
+    for (int i = 0; i < 8; i++) {
+        const uint32_t c = rnd == ROUND_TOWARD_ZERO ? encode_elem<FMT, ROUND_TOWARD_ZERO>(r[0], s)
+                           : rnd == ROUND_HALF_AWAY ? encode_elem<FMT, ROUND_HALF_AWAY>(r[0], s) : encode_elem<FMT, ROUND_RNE>(r[0], s);
+        bits = (bits >> w) | ((uint64_t)c << (7 * w));
+#pragma unroll
+        for (int j = 0; j < 7; j++) r[j] = r[j + 1];
+    }
     out[0] = (uint32_t)bits;
     out[1] = (uint32_t)(bits >> 32);
     return s;

@@ -3,8 +3,8 @@
 // dx is the gradient of x and of the residual alike; dh is the gradient that reaches h past the layer.
 // Bound by memory: dy, h (and dh) read and dx written, once; everything else is small.
 //
-// norm_bwd_kernel: a fixed number of work-groups walks the rows; a row lies in the registers of NT threads (a wave, or the
-// work-group) as packed pairs, the weight is kept unpacked from row to row, and every thread adds up its own columns'
+// norm_bwd_kernel: a number of work-groups that the shape fixes walks the rows; a row lies in registers, a vector of eight columns a thread
+// (two beyond 8192 columns; a wave a row up to 512), the weight is kept from row to row, and every thread adds up its own columns'
 // part of dweight in Float32.  Each work-group writes one line of partial sums to scratch memory and
 // norm_bwd_weight_kernel adds the lines in a fixed order: no atomics, the same bits every time.
 // norm_bwd_long_kernel and norm_bwd_long_weight_kernel: rows that do not fit in registers; dy and h are read three times.
@@ -72,39 +72,47 @@ __device__ __forceinline__ void load_weight(const NormBwdArgs &a, int64_t col, i
     }
 }
 
-template <int DT, int NT, int VPT>
-__global__ __launch_bounds__(256) void norm_bwd_kernel(NormBwdArgs a)
+template <int DT, int VPT, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_bwd_kernel(NormBwdArgs a)
 {
-    constexpr int RPW = 256 / NT;
-    __shared__ float lds[NT == 64 ? 256 * 8 : 2 * (NT / 64)];
-    const int t = threadIdx.x & (NT - 1);
+    __shared__ float lds[WAVE ? 256 * 8 : 2 * 16];
+    const int nt = WAVE ? 64 : (int)blockDim.x, t = WAVE ? threadIdx.x & 63 : threadIdx.x;
+    constexpr int RPW = WAVE ? 4 : 1;                 // rows a work-group has in hand
     float w[VPT][8], dw[VPT][8];
 #pragma unroll
     for (int k = 0; k < VPT; k++) {
-        const int64_t col = (int64_t)(k * NT + t) * 8;
+        const int64_t col = (int64_t)(k * nt + t) * 8;
         load_weight(a, col, inside(a.cols - col, 8), w[k]);
 #pragma unroll
         for (int i = 0; i < 8; i++) dw[k][i] = 0.0f;
     }
     const float inv = 1.0f / (float)a.cols;
-    int trip = 0;
-    for (int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / NT; row < a.rows; row += (int64_t)gridDim.x * RPW, trip ^= 1) {
-        Vec8<DT> dy[VPT], h[VPT], dh[VPT];
+    const int64_t first = (int64_t)blockIdx.x * RPW + (WAVE ? threadIdx.x >> 6 : 0), pitch = (int64_t)gridDim.x * RPW;
+    // a row's vectors and its rstd, requested one row ahead: the sum over a row, and the barrier in it, would leave the memory idle (4096 x
+    // 8192 bf16 58 us without, 51 with).  Two vectors a thread leave no registers for that in a work-group of 1024.
+    constexpr bool AHEAD = VPT == 1;
+    Vec8<DT> dy1[VPT], h1[VPT], dh1[VPT];
+    float rstd1 = 0.0f;
+    auto request = [&](int64_t row) __attribute__((always_inline)) {
 #pragma unroll
         for (int k = 0; k < VPT; k++) {
-            const int64_t col = (int64_t)(k * NT + t) * 8;
+            const int64_t col = (int64_t)(k * nt + t) * 8;
             const int n = inside(a.cols - col, 8);
-            dy[k] = fetch8<DT>(a.dy, row * a.lddy + col, n);
-            h[k] = fetch8<DT>(a.h, row * a.ldh + col, n);
+            dy1[k] = fetch8<DT>(a.dy, row * a.lddy + col, n);
+            h1[k] = fetch8<DT>(a.h, row * a.ldh + col, n);
+            if (a.dh) dh1[k] = fetch8<DT>(a.dh, row * a.lddh + col, n);
         }
-        const float rstd = a.rstd[row];
-        if (a.dh) {
+        rstd1 = a.rstd[row];
+    };
+    if (AHEAD && first < a.rows) request(first);
+    int trip = 0;
+    for (int64_t row = first; row < a.rows; row += pitch, trip ^= 1) {
+        if (!AHEAD) request(row);
+        Vec8<DT> dy[VPT], h[VPT], dh[VPT];
 #pragma unroll
-            for (int k = 0; k < VPT; k++) {
-                const int64_t col = (int64_t)(k * NT + t) * 8;
-                dh[k] = fetch8<DT>(a.dh, row * a.lddh + col, inside(a.cols - col, 8));
-            }
-        }
+        for (int k = 0; k < VPT; k++) { dy[k] = dy1[k]; h[k] = h1[k]; dh[k] = dh1[k]; }
+        const float rstd = rstd1;
+        if (AHEAD && row + pitch < a.rows) request(row + pitch);
         float sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < VPT; k++)
@@ -114,11 +122,11 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormBwdArgs a)
                 sum = fmaf(d * w[k][i], x, sum);
                 dw[k][i] = fmaf(d, x, dw[k][i]);
             }
-        // (two places in LDS taken in turn: a barrier in between keeps a fast wave from writing where a slow one still reads)
-        const float mean = row_sum<NT>(sum, lds + (NT == 64 ? 0 : trip * (NT / 64))) * inv;
+        // (two places in LDS taken in turn: the barrier in between keeps a fast wave from writing where a slow one still reads)
+        const float mean = row_sum<WAVE>(sum, lds + (WAVE ? 0 : trip * 16)) * inv;
 #pragma unroll
         for (int k = 0; k < VPT; k++) {
-            const int64_t col = (int64_t)(k * NT + t) * 8;
+            const int64_t col = (int64_t)(k * nt + t) * 8;
             const int n = inside(a.cols - col, 8);
             float dx[8];
 #pragma unroll
@@ -137,10 +145,9 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormBwdArgs a)
     float *line = a.partial + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
     for (int k = 0; k < VPT; k++) {
-        const int64_t col = (int64_t)(k * NT + t) * 8;
+        const int64_t col = (int64_t)(k * nt + t) * 8;
         const int n = inside(a.cols - col, 8);
-        if constexpr (NT == 64) {                     // four rows at a time: their waves' sums in order
-            if (k > 0) __syncthreads();
+        if constexpr (WAVE) {                         // four rows at a time: their waves' sums in order
 #pragma unroll
             for (int i = 0; i < 8; i++) lds[threadIdx.x * 8 + i] = dw[k][i];
             __syncthreads();
@@ -159,28 +166,29 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormBwdArgs a)
     }
 }
 
-// dweight[c] = partial[0][c] + partial[1][c] + ..., 16 columns and 16 runs of lines a work-group
-__global__ __launch_bounds__(256) void norm_bwd_weight_kernel(const float *__restrict__ partial, int lines, int64_t cols, float *__restrict__ dweight)
+// dweight[c] = partial[0][c] + partial[1][c] + ..., 16 columns and 64 runs of lines a work-group
+__global__ __launch_bounds__(1024) void norm_bwd_weight_kernel(const float *__restrict__ partial, int lines, int64_t cols, float *__restrict__ dweight)
 {
-    __shared__ float part[16][17];
+    __shared__ float part[64][17];
     const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
     const int64_t col = (int64_t)blockIdx.x * 16 + c;
     float sum = 0.0f;
     if (col < cols) {
         int l = g;
-        for (; l + 112 < lines; l += 128) {
+        for (; l + 448 < lines; l += 512) {
             float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) v[j] = partial[(int64_t)(l + 16 * j) * cols + col];
+            for (int j = 0; j < 8; j++) v[j] = partial[(int64_t)(l + 64 * j) * cols + col];
 #pragma unroll
             for (int j = 0; j < 8; j++) sum += v[j];
         }
-        for (; l < lines; l += 16) sum += partial[(int64_t)l * cols + col];
+        for (; l < lines; l += 64) sum += partial[(int64_t)l * cols + col];
     }
     part[g][c] = sum;
     __syncthreads();
-    if (g == 0 && col < cols) {
-        for (int j = 1; j < 16; j++) sum += part[j][c];
+    if (threadIdx.x < 16 && col < cols) {
+        sum = 0.0f;
+        for (int j = 0; j < 64; j++) sum += part[j][c];
         dweight[col] = sum;
     }
 }
@@ -200,7 +208,7 @@ __global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
 #pragma unroll
         for (int i = 0; i < 8; i++) sum = fmaf(elem<DT>(dy, i) * w[i], elem<DT>(h, i) * rstd, sum);
     }
-    const float mean = row_sum<256>(sum, lds) / (float)a.cols;
+    const float mean = row_sum<false>(sum, lds) / (float)a.cols;
     for (int64_t col = threadIdx.x * 8; col < a.cols; col += 2048) {
         const int n = inside(a.cols - col, 8);
         float w[8], dx[8];
@@ -237,14 +245,20 @@ __global__ __launch_bounds__(256) void norm_bwd_long_weight_kernel(NormBwdArgs a
         if (i < n) line[col + i] = dw[i];
 }
 
-// Columns that fit in registers: 8192 for a work-group.
-constexpr int64_t NORM_BWD_COLS = 8192;
+// Columns that fit in registers, and threads of a work-group for so many
+constexpr int64_t NORM_BWD_COLS = 16384;
+static int norm_bwd_threads(int64_t cols)
+{
+    const int64_t nvec = (cols + 7) / 8;
+    return nvec <= 64 ? 256 : nvec <= 1024 ? (int)((nvec + 63) / 64 * 64) : (int)((nvec + 127) / 128 * 64);
+}
 
-// Lines of partial sums: as many work-groups as the chip holds two of per compute unit, fewer where there are fewer rows.
+// Lines of partial sums: as many work-groups as give each compute unit 512 threads, one at least, fewer where there are fewer rows.  (16384 x 2048
+// bf16 50.5 us so, 53.7 with 1024 threads, 60 with 2048; 8192 x 4096 49.7, 51.4, 58.)
 int norm_bwd_lines(int64_t rows, int64_t cols)
 {
-    const int64_t need = cols > NORM_BWD_COLS ? rows : cols <= 2048 ? (rows + 3) / 4 : rows;
-    const int64_t most = cols > NORM_BWD_COLS ? 64 : 512;
+    if (cols > NORM_BWD_COLS) return (int)(rows < 64 ? rows : 64);
+    const int64_t need = cols <= 512 ? (rows + 3) / 4 : rows, threads = norm_bwd_threads(cols), most = threads < 512 ? 256 * (512 / threads) : 256;
     return (int)(need < most ? need : most);
 }
 
@@ -263,19 +277,14 @@ static hipError_t launch_norm_bwd_t(const NormBwdArgs &a, int lines, float *dwei
         if (a.partial)                                // first: dx may take the place of dy
             hipLaunchKernelGGL((norm_bwd_long_weight_kernel<DT>), dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)lines), b, 0, st, a);
         hipLaunchKernelGGL((norm_bwd_long_kernel<DT>), dim3((unsigned)a.rows), b, 0, st, a);
-    } else if (a.cols <= 512) {
-        hipLaunchKernelGGL((norm_bwd_kernel<DT, 64, 1>), g, b, 0, st, a);
-    } else if (a.cols <= 1024) {
-        hipLaunchKernelGGL((norm_bwd_kernel<DT, 64, 2>), g, b, 0, st, a);
-    } else if (a.cols <= 2048) {
-        hipLaunchKernelGGL((norm_bwd_kernel<DT, 64, 4>), g, b, 0, st, a);
-    } else if (a.cols <= 4096) {
-        hipLaunchKernelGGL((norm_bwd_kernel<DT, 256, 2>), g, b, 0, st, a);
     } else {
-        hipLaunchKernelGGL((norm_bwd_kernel<DT, 256, 4>), g, b, 0, st, a);
+        const dim3 threads(norm_bwd_threads(a.cols));
+        if (a.cols <= 512) hipLaunchKernelGGL((norm_bwd_kernel<DT, 1, true>), g, threads, 0, st, a);
+        else if (a.cols <= 8192) hipLaunchKernelGGL((norm_bwd_kernel<DT, 1, false>), g, threads, 0, st, a);
+        else hipLaunchKernelGGL((norm_bwd_kernel<DT, 2, false>), g, threads, 0, st, a);
     }
     if (a.partial)
-        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((a.cols + 15) / 16)), b, 0, st, a.partial, lines, a.cols, dweight);
+        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((a.cols + 15) / 16)), dim3(1024), 0, st, a.partial, lines, a.cols, dweight);
     return hipGetLastError();
 }
 
@@ -284,7 +293,7 @@ hipError_t launch_norm_bwd(const void *dy, int64_t lddy, const void *h, int64_t 
 {
     NormBwdArgs a = {dy, h, weight, dh, rstd, dx, nullptr, rows, cols, lddy, ldh, lddh, lddx, w_dt};
     if (rows == 0) {                                  // an empty sum
-        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(256), 0, st, a.partial, 0, cols, dweight);
+        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, st, a.partial, 0, cols, dweight);
         return hipGetLastError();
     }
     uint8_t *ws = nullptr;

@@ -4,9 +4,11 @@
 // Float32 scale per 128.  (h w first: for bf16 h and w that product is exact, so y carries one rounding and that of rstd.)
 // Bound by memory: x and the residual read, h and the codes written, all once.
 //
-// norm_kernel: a row stays in the registers of NT threads, VPT vectors of eight elements each, between the sum of squares and the output; NT = 64: a wave a
-// row and no barrier, four rows a work-group; NT = 256: the work-group a row.  norm_long_kernel: rows that do not fit; h is read
-// (or added up) a second time.
+// norm_kernel: a row stays in registers between the sum of squares and the output: a vector of eight elements a thread and as many threads as
+// that takes, two vectors beyond 8192 columns, and for up to 512 columns a wave a row, four rows a work-group.  More vectors a thread and
+// fewer threads are slower throughout: 8192 x 4096 bf16 with a residual 44 us with one (512 threads), 45 with two, 48 with four, 58 with eight
+// (a wave a row); one row of 4096 3.0, 3.9, 5.6 and 8.9; 2048 x 16384 46 with two vectors, 48 with four, 57 with eight.
+// norm_long_kernel: rows beyond 16384 columns; h is read (or added up) a second time.
 #pragma once
 
 #include "mx_norm.hpp"
@@ -47,43 +49,42 @@ __device__ __forceinline__ void put_vector(const NormArgs &a, int64_t row, int v
     put_cast<OUT>(y, a.rnd, a.elems, a.scales, row, vec, a.nvec, on);
 }
 
-template <int OUT, int DT, int NT, int VPT>
-__global__ __launch_bounds__(256) void norm_kernel(NormArgs a)
+template <int OUT, int DT, int VPT, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a)
 {
     norm_modes<OUT>();
-    __shared__ float lds[NT / 64];
-    constexpr int RPW = 256 / NT;                     // rows a work-group
-    const int t = threadIdx.x & (NT - 1);
-    const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / NT;
-    if (NT == 64 && row >= a.rows) return;            // (a whole wave; the kernel has no barrier then)
+    __shared__ float lds[16];
+    const int nt = WAVE ? 64 : (int)blockDim.x, t = WAVE ? threadIdx.x & 63 : threadIdx.x;
+    const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+    if (WAVE && row >= a.rows) return;                // (a whole wave; the kernel has no barrier then)
     float h[VPT][8], sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < VPT; k++) {
-        const int64_t col = (int64_t)(k * NT + t) * 8;
+        const int64_t col = (int64_t)(k * nt + t) * 8;
         load_sum<DT>(a, row, col, inside(a.cols - col, 8), h[k]);
     }
 #pragma unroll
     for (int k = 0; k < VPT; k++) {
-        const int64_t col = (int64_t)(k * NT + t) * 8;
+        const int64_t col = (int64_t)(k * nt + t) * 8;
         const int n = inside(a.cols - col, 8);
         if (a.h && n > 0) put8<DT>(a.h, row * a.ldh + col, n, h[k]);
 #pragma unroll
         for (int i = 0; i < 8; i++) sum = fmaf(h[k][i], h[k][i], sum);
     }
-    const float rstd = rsqrtf(row_sum<NT>(sum, lds) / (float)a.cols + a.eps);
+    const float rstd = rsqrtf(row_sum<WAVE>(sum, lds) / (float)a.cols + a.eps);
     if (a.rstd && t == 0) a.rstd[row] = rstd;
 #pragma unroll
-    for (int k = 0; k < VPT; k++) put_vector<OUT, DT>(a, row, k * NT + t, k * NT + t < a.nvec, h[k], rstd);
+    for (int k = 0; k < VPT; k++) put_vector<OUT, DT>(a, row, k * nt + t, k * nt + t < a.nvec, h[k], rstd);
 }
 
 template <int OUT, int DT>
-__global__ __launch_bounds__(256) void norm_long_kernel(NormArgs a)
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
 {
     norm_modes<OUT>();
-    __shared__ float lds[4];
+    __shared__ float lds[16];
     const int64_t row = blockIdx.x;
     float sum = 0.0f;
-    for (int vec = threadIdx.x; vec < a.nvec; vec += 256) {
+    for (int vec = threadIdx.x; vec < a.nvec; vec += 1024) {
         const int64_t col = (int64_t)vec * 8;
         const int n = inside(a.cols - col, 8);
         float h[8];
@@ -92,11 +93,11 @@ __global__ __launch_bounds__(256) void norm_long_kernel(NormArgs a)
 #pragma unroll
         for (int i = 0; i < 8; i++) sum = fmaf(h[i], h[i], sum);
     }
-    const float rstd = rsqrtf(row_sum<256>(sum, lds) / (float)a.cols + a.eps);
+    const float rstd = rsqrtf(row_sum<false>(sum, lds) / (float)a.cols + a.eps);
     if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
-    const int trips = (a.nvec + 255) / 256;           // (the same number for every lane: they share blocks)
+    const int trips = (a.nvec + 1023) / 1024;           // (the same number for every lane: they share blocks)
     for (int k = 0; k < trips; k++) {
-        const int vec = k * 256 + threadIdx.x;
+        const int vec = k * 1024 + threadIdx.x;
         const bool on = vec < a.nvec;
         const int64_t col = (int64_t)vec * 8;
         const int n = on ? inside(a.cols - col, 8) : 0;
@@ -108,22 +109,14 @@ __global__ __launch_bounds__(256) void norm_long_kernel(NormArgs a)
     }
 }
 
-// Which form: a wave a row up to 4096 columns where there are rows enough to fill the chip with waves, else the work-group.
 template <int OUT, int DT>
 static hipError_t launch_norm_t(const NormArgs &a, hipStream_t st)
 {
-    const int64_t most = ((int64_t)1 << 31) - 1;
-    const bool waves = a.nvec <= 512 && a.rows >= 1024;
-    const int64_t grid = waves ? (a.rows + 3) / 4 : a.rows;
-    if (grid > most) return hipErrorNotSupported;
-    const dim3 g((unsigned)grid), b(256);
-    if (waves && a.nvec <= 128) hipLaunchKernelGGL((norm_kernel<OUT, DT, 64, 2>), g, b, 0, st, a);
-    else if (waves && a.nvec <= 256) hipLaunchKernelGGL((norm_kernel<OUT, DT, 64, 4>), g, b, 0, st, a);
-    else if (waves) hipLaunchKernelGGL((norm_kernel<OUT, DT, 64, 8>), g, b, 0, st, a);
-    else if (a.nvec <= 512) hipLaunchKernelGGL((norm_kernel<OUT, DT, 256, 2>), g, b, 0, st, a);
-    else if (a.nvec <= 1024) hipLaunchKernelGGL((norm_kernel<OUT, DT, 256, 4>), g, b, 0, st, a);
-    else if (a.nvec <= 2048) hipLaunchKernelGGL((norm_kernel<OUT, DT, 256, 8>), g, b, 0, st, a);
-    else hipLaunchKernelGGL((norm_long_kernel<OUT, DT>), g, b, 0, st, a);
+    const int threads = a.nvec <= 1024 ? (a.nvec + 63) / 64 * 64 : a.nvec <= 2048 ? (a.nvec + 127) / 128 * 64 : 1024;
+    if (a.nvec <= 64) hipLaunchKernelGGL((norm_kernel<OUT, DT, 1, true>), dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, st, a);
+    else if (a.nvec <= 1024) hipLaunchKernelGGL((norm_kernel<OUT, DT, 1, false>), dim3((unsigned)a.rows), dim3(threads), 0, st, a);
+    else if (a.nvec <= 2048) hipLaunchKernelGGL((norm_kernel<OUT, DT, 2, false>), dim3((unsigned)a.rows), dim3(threads), 0, st, a);
+    else hipLaunchKernelGGL((norm_long_kernel<OUT, DT>), dim3((unsigned)a.rows), dim3(threads), 0, st, a);
     return hipGetLastError();
 }
 
