@@ -35,18 +35,18 @@ __device__ __forceinline__ uint32_t row16_max(uint32_t v)
     o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140 /* row_mirror */, 0xF, 0xF, false);
     return v > o ? v : o;
 }
-// ... of 32 and of 64 adjacent lanes
+// ... of 32 and of 64 adjacent lanes: the row swaps leave a row's and its neighbour's value in one lane of either result
 __device__ __forceinline__ uint32_t row32_max(uint32_t v)
 {
     v = row16_max(v);
-    const uint32_t o = (uint32_t)__shfl_xor((int)v, 16);
-    return v > o ? v : o;
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return r[0] > r[1] ? r[0] : r[1];
 }
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
     v = row32_max(v);
-    const uint32_t o = (uint32_t)__shfl_xor((int)v, 32);
-    return v > o ? v : o;
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return r[0] > r[1] ? r[0] : r[1];
 }
 
 // N Float32 values (bit patterns), all finite, times factor -> N codes, four to a dword.  The wave is in fp8_saturate_mode().

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void dequant128_col_kernel(const uint8_t *__re
                                                              int64_t rows, int64_t cols, int64_t ld, int64_t n_rb, int64_t n_tiles, int64_t per_xcd,
                                                              void *__restrict__ dst)
 {
-    constexpr int PITCH = BLOCK128 + 16;              // bytes per line: 16-byte writes, and dword reads of eight lines that meet different banks
+    constexpr int PITCH = BLOCK128 + 4;               // bytes per line: the dword reads below, 4 or 8 lines and consecutive dwords apart, meet 64 banks
     __shared__ __attribute__((aligned(16))) uint8_t tile[64 * PITCH];
     __shared__ float sc[64];
     const int64_t tile_id = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
@@ -110,7 +110,8 @@ __global__ __launch_bounds__(256) void dequant128_col_kernel(const uint8_t *__re
         const int64_t col = cs * 64 + line;
         uint4 d = make_uint4(0, 0, 0, 0);
         if (col < cols) d = ld16_nt(elems + (col * n_rb + tr) * BLOCK128 + (t & 7) * 16);
-        *reinterpret_cast<uint4 *>(tile + line * PITCH + (t & 7) * 16) = d;
+        uint32_t *o = reinterpret_cast<uint32_t *>(tile + line * PITCH + (t & 7) * 16);
+        o[0] = d.x; o[1] = d.y; o[2] = d.z; o[3] = d.w;
     }
     if (t < 64) sc[t] = cs * 64 + t < cols ? scales[((cs * 64 + t) >> tile_shift) * n_rb + tr] : 0.0f;
     __syncthreads();

@@ -1,6 +1,8 @@
 // What the RMS norm kernels share: eight consecutive elements of a row per lane and vector.
 #pragma once
 
+#include <type_traits>
+
 #include "mx_b128.hpp"
 #include "mx_launch.hpp"
 
@@ -72,13 +74,24 @@ __device__ __forceinline__ float held(float v) { return DT == DT_BF16 ? __uint_a
 
 __device__ __forceinline__ int inside(int64_t left, int n) { return left >= n ? n : left > 0 ? (int)left : 0; }
 
+// The sum over groups of 16 lanes, and over a wave, in every lane (in one order for all of them)
+__device__ __forceinline__ float row16_sum(float v)
+{
+    auto from = [](float x, auto ctrl) { return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, false)); };
+    v += from(v, std::integral_constant<int, 0xB1>());      // quad_perm [1,0,3,2]
+    v += from(v, std::integral_constant<int, 0x4E>());      // quad_perm [2,3,0,1]
+    v += from(v, std::integral_constant<int, 0x141>());     // row_half_mirror
+    return v + from(v, std::integral_constant<int, 0x140>());   // row_mirror
+}
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    v = row16_sum(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-// The sum over the threads that share a row, in each of them: a wave, or the work-group by way of LDS (a float for each of its waves).
+// The sum over the threads that share a row, in each of them: a wave, or the work-group by way of LDS (a float for each of its waves, 16 at most).
 template <bool WAVE>
 __device__ __forceinline__ float row_sum(float v, float *lds)
 {
@@ -86,9 +99,8 @@ __device__ __forceinline__ float row_sum(float v, float *lds)
     if constexpr (!WAVE) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = lds[0];
-        const int waves = (int)blockDim.x >> 6;
-        for (int i = 1; i < waves; i++) v += lds[i];
+        const int i = threadIdx.x & 15;
+        v = row16_sum(i < (int)blockDim.x >> 6 ? lds[i] : 0.0f);
     }
     return v;
 }
