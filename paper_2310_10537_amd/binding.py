@@ -436,41 +436,40 @@ def mx_dequantize_3d(elems, scales, fmt, shape, axis, keep_order=False, dtype=to
 BLOCK128 = 128
 
 
-class _On:
-    """The device of a call's tensors made the current one, and the stream that the call runs on: the given one, else torch's current
-    stream of that device."""
-    __slots__ = ("guard", "stream")
-
-    def __init__(self, device, stream):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return ctypes.c_void_p(self.stream.cuda_stream)
-
-    def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
+def _call(device, stream, fn, *args):
+    """A library function on the device of a call's tensors and on the given stream, else torch's current one of that device."""
+    index = device.index
+    raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
+    if index == torch.cuda.current_device():
+        status = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, raw)
+    if status != MX_OK:
+        _check(status)
 
 
 def _rows(t, name, like=None):
     """Pitch (elements) of a 2-D float32 / bfloat16 device tensor whose rows are contiguous; `like`: it has that tensor's shape, type and device."""
-    _dev(t, name)
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in device memory")
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError(f"{name} must be a matrix with contiguous rows")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+    pitch, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    if like is not None and (shape != like.shape or t.dtype != like.dtype or t.device != like.device):
         raise ValueError(f"{name} must have the shape {tuple(like.shape)}, type and device of the tensor it goes with")
-    if t.shape[0] > 1:
-        return t.stride(0)
+    if shape[0] > 1:
+        return pitch
     per16 = 16 // t.element_size()
-    return -(-t.shape[1] // per16) * per16            # one row: its pitch is never used, but has to be a possible one
+    return -(-shape[1] // per16) * per16              # one row: its pitch is never used, but has to be a possible one
 
 
 def _flat(t, name, shape, dtype, device):
     """A contiguous tensor of exactly this shape and type."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {device}")
     return t
 
@@ -490,8 +489,7 @@ def mx_quantize_b128(src, axis, fmt, tile=False, elems_out=None, scales_out=None
     shape_e, shape_s = _b128_shapes(rows, cols, axis, tile)
     elems = torch.empty(shape_e, dtype=torch.uint8, device=src.device) if elems_out is None else _flat(elems_out, "elems_out", shape_e, torch.uint8, src.device)
     scales = torch.empty(shape_s, dtype=torch.float32, device=src.device) if scales_out is None else _flat(scales_out, "scales_out", shape_s, torch.float32, src.device)
-    with _On(src.device, stream) as st:
-        _check(lib().mx_quantize_b128(src.data_ptr(), dt, rows, cols, ld, axis, 1 if tile else 0, fmt, elems.data_ptr(), scales.data_ptr(), st))
+    _call(src.device, stream, lib().mx_quantize_b128, src.data_ptr(), dt, rows, cols, ld, axis, 1 if tile else 0, fmt, elems.data_ptr(), scales.data_ptr())
     return elems, scales
 
 
@@ -506,14 +504,13 @@ def mx_dequantize_b128(elems, scales, fmt, rows, cols, axis, tile=False, dtype=t
     elif tuple(out.shape) != (rows, cols) or out.device != elems.device:
         raise ValueError(f"out must be a [{rows}, {cols}] tensor on {elems.device}")
     ld = _rows(out, "out")
-    with _On(elems.device, stream) as st:
-        _check(lib().mx_dequantize_b128(elems.data_ptr(), scales.data_ptr(), fmt, rows, cols, axis, 1 if tile else 0, out.data_ptr(), _dt(out), ld, st))
+    _call(elems.device, stream, lib().mx_dequantize_b128, elems.data_ptr(), scales.data_ptr(), fmt, rows, cols, axis, 1 if tile else 0, out.data_ptr(), _dt(out), ld)
     return out
 
 
 def _empty_rows(rows, cols, dtype, device):
     """A matrix whose rows start at multiples of 16 bytes."""
-    per16 = 16 // torch.empty((), dtype=dtype).element_size()
+    per16 = 8 if dtype == torch.bfloat16 else 4
     if cols % per16 == 0 or rows <= 1:
         return torch.empty((rows, cols), dtype=dtype, device=device)
     return torch.empty((rows, -(-cols // per16) * per16), dtype=dtype, device=device)[:, :cols]
@@ -541,9 +538,8 @@ def mx_gemm_b128(A_elems, A_scales, fmtA, B_elems, B_scales, fmtB, K, dtype=torc
     elif tuple(out.shape) != (M, N) or out.device != A_elems.device or (N > 1 and out.stride(1) != 1):
         raise ValueError(f"out must be a [{M}, {N}] tensor with contiguous rows on {A_elems.device}")
     ldc = out.stride(0) if M > 1 else N
-    with _On(A_elems.device, stream) as st:
-        _check(lib().mx_gemm_b128(M, N, K, A_elems.data_ptr(), A_scales.data_ptr(), tileA, fmtA, B_elems.data_ptr(), B_scales.data_ptr(), tileB, fmtB,
-                                  out.data_ptr(), _dt(out), ldc, st))
+    _call(A_elems.device, stream, lib().mx_gemm_b128, M, N, K, A_elems.data_ptr(), A_scales.data_ptr(), tileA, fmtA, B_elems.data_ptr(), B_scales.data_ptr(), tileB, fmtB,
+          out.data_ptr(), _dt(out), ldc)
     return out
 
 
@@ -575,8 +571,7 @@ def mx_rmsnorm(x, weight, eps, residual=None, h_out=None, y_out=None, rstd_out=N
         _rows(x, "x")
         y_out = _empty_rows(x.shape[0], x.shape[1], x.dtype, x.device)
     head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
-    with _On(x.device, stream) as st:
-        _check(lib().mx_rmsnorm(*head, *tail, st))
+    _call(x.device, stream, lib().mx_rmsnorm, *head, *tail)
     return y_out
 
 
@@ -588,8 +583,7 @@ def mx_rmsnorm_q(x, weight, eps, fmt, rnd=ROUND_RNE, residual=None, h_out=None, 
     width = blocks * BLOCK * (FORMAT_BITS[fmt] if 0 <= fmt < 6 else 8) // 8
     elems = torch.empty((rows, width), dtype=torch.uint8, device=x.device) if elems_out is None else _flat(elems_out, "elems_out", (rows, width), torch.uint8, x.device)
     scales = torch.empty((rows, blocks), dtype=torch.uint8, device=x.device) if scales_out is None else _flat(scales_out, "scales_out", (rows, blocks), torch.uint8, x.device)
-    with _On(x.device, stream) as st:
-        _check(lib().mx_rmsnorm_q(*head, fmt, rnd, elems.data_ptr(), scales.data_ptr(), *tail, st))
+    _call(x.device, stream, lib().mx_rmsnorm_q, *head, fmt, rnd, elems.data_ptr(), scales.data_ptr(), *tail)
     return elems, scales
 
 
@@ -599,8 +593,7 @@ def mx_rmsnorm_b128(x, weight, eps, fmt, residual=None, h_out=None, y_out=None, 
     shape_e, shape_s = _b128_shapes(x.shape[0], x.shape[1], 1, False)
     elems = torch.empty(shape_e, dtype=torch.uint8, device=x.device) if elems_out is None else _flat(elems_out, "elems_out", shape_e, torch.uint8, x.device)
     scales = torch.empty(shape_s, dtype=torch.float32, device=x.device) if scales_out is None else _flat(scales_out, "scales_out", shape_s, torch.float32, x.device)
-    with _On(x.device, stream) as st:
-        _check(lib().mx_rmsnorm_b128(*head, fmt, elems.data_ptr(), scales.data_ptr(), *tail, st))
+    _call(x.device, stream, lib().mx_rmsnorm_b128, *head, fmt, elems.data_ptr(), scales.data_ptr(), *tail)
     return elems, scales
 
 
@@ -619,20 +612,19 @@ def mx_rmsnorm_bwd(dy, h, weight, rstd, dh=None, dx_out=None, want_dweight=True,
     dx = _empty_rows(rows, cols, dy.dtype, dy.device) if dx_out is None else dx_out
     lddx = _rows(dx, "dx_out", dy)
     dweight = torch.empty((cols,), dtype=torch.float32, device=dy.device) if want_dweight else None
-    with _On(dy.device, stream) as st:
-        ws = _bwd_workspace(rows, cols, dy.device, stream) if want_dweight else None
-        wp, wb = _ws_args(ws)
-        _check(lib().mx_rmsnorm_bwd_ws(dy.data_ptr(), ldy, h.data_ptr(), ldh, None if weight is None else weight.data_ptr(), w_dt, rstd.data_ptr(),
-                                       None if dh is None else dh.data_ptr(), lddh, _dt(dy), rows, cols, dx.data_ptr(), lddx,
-                                       None if dweight is None else dweight.data_ptr(), wp, wb, st))
+    ws = _bwd_workspace(rows, cols, dy.device, stream) if want_dweight else None
+    wp, wb = _ws_args(ws)
+    _call(dy.device, stream, lib().mx_rmsnorm_bwd_ws, dy.data_ptr(), ldy, h.data_ptr(), ldh, None if weight is None else weight.data_ptr(), w_dt, rstd.data_ptr(),
+          None if dh is None else dh.data_ptr(), lddh, _dt(dy), rows, cols, dx.data_ptr(), lddx, None if dweight is None else dweight.data_ptr(), wp, wb)
     return dx, dweight
 
 
 def _bwd_workspace(rows, cols, device, stream):
     """The partial sums' scratch memory from torch's caching allocator, or None for the library's own: as for the products, on torch's current
     stream only, and not while it is captured."""
-    current = torch.cuda.current_stream()
-    if (stream is not None and stream.cuda_stream != current.cuda_stream) or torch.cuda.is_current_stream_capturing():
+    if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(device.index):
+        return None
+    if torch.cuda.is_current_stream_capturing():
         return None
     need = lib().mx_rmsnorm_bwd_workspace_bytes(rows, cols)
     try:
