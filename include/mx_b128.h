@@ -46,8 +46,8 @@ size_t mx_b128_scale_count(int64_t rows, int64_t cols, int axis, int tile);
  *              or infinity (E5M2).
  * (The cut makes v * factor exact for bf16 v.  A block of zeros gets scale 2^-126.)
  * Outputs are 16-byte aligned, of the sizes above.
- * MX_ERR_UNSUPPORTED: more than 2^31 - 8 tiles of 128 x 128, or lines longer than
- * about 2^33 elements.
+ * MX_ERR_UNSUPPORTED: more than about 2^24 tiles of 128 x 128 (with axis 0 or tile
+ * 1), or rows longer than about 2^33 elements (else).
  */
 int mx_quantize_b128(const void *src, mx_dtype_t src_dt, int64_t rows, int64_t cols,
                      int64_t ld, int axis, int tile, mx_format_t fmt,
@@ -55,7 +55,8 @@ int mx_quantize_b128(const void *src, mx_dtype_t src_dt, int64_t rows, int64_t c
 
 /* elems * scales, rounded to Float32 and from there to dst_dt, into the row-major
  * dst [rows, cols] with leading dimension ld; arguments as mx_dequantize.  The fill
- * of a partial last block is skipped. */
+ * of a partial last block is skipped.  MX_ERR_UNSUPPORTED: as above, with axis 0
+ * more than about 2^24 tiles of 128 x 64. */
 int mx_dequantize_b128(const void *elems, const float *scales, mx_format_t fmt,
                        int64_t rows, int64_t cols, int axis, int tile,
                        void *dst, mx_dtype_t dst_dt, int64_t ld, void *hip_stream);
@@ -79,7 +80,8 @@ int mx_dequantize_b128(const void *elems, const float *scales, mx_format_t fmt,
  * results are reproducible.
  * C, c_dt, ldc, alignment as mx_gemm (scales 16-byte aligned too).  rows of C beyond
  * M and columns beyond N are not touched.
- * MX_ERR_UNSUPPORTED: more than 2^30 tiles of C, or K of 2^38 and more.
+ * MX_ERR_UNSUPPORTED: more than 2^22 tiles of C (of 128 x 128 at least), N of 2^27
+ * and more with M up to 64, or K of 2^38 and more.
  */
 int mx_gemm_b128(int64_t M, int64_t N, int64_t K,
                  const void *A_elems, const float *A_scales, int tileA, mx_format_t fmtA,

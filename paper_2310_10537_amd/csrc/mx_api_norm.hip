@@ -35,7 +35,7 @@ int rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const
     const int64_t block = mx::out_block(out);
     if (rows >= (int64_t)1 << 31 || cols >= (int64_t)1 << 32) return MX_ERR_UNSUPPORTED;
     const mx::NormArgs a = {x, residual, weight, h, y, static_cast<uint8_t *>(elems), scales, rstd, rows, cols, ldx, ldr, ldh, ldy, eps,
-                            w_dt, rnd, (int)((cols + block - 1) / block * (block / 8))};
+                            w_dt, rnd, (int)((cols + block - 1) / block * (block / 8)), 0};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return status(dt == MX_DT_BF16 ? mx::launch_norm_bf16(a, out, st) : mx::launch_norm_f32(a, out, st));
 }

@@ -291,8 +291,8 @@ static hipError_t launch_cast128_t(const void *src, int64_t rows, int64_t cols, 
         }
         return hipGetLastError();
     }
-    // one work-group a tile
-    if (n_rb > (((int64_t)1 << 31) - 8) / n_cb) return hipErrorNotSupported;
+    // one work-group a tile; the runtime counts a grid's threads in 32 bits
+    if (n_rb > (((int64_t)1 << 24) - 8) / n_cb) return hipErrorNotSupported;
     const int64_t n_tiles = n_rb * n_cb, per_xcd = (n_tiles + 7) / 8;
     if (axis == 1)
         hipLaunchKernelGGL((cast128_tile_kernel<FMT, DT>), dim3((unsigned)n_tiles), dim3(256), 0, st, src, rows, cols, ld, elems, scales, n_cb);

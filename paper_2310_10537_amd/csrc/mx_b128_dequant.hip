@@ -164,7 +164,7 @@ static hipError_t launch_dequant128_t(const uint8_t *elems, const float *scales,
         return hipGetLastError();
     }
     const int64_t n_cs = (cols + 63) / 64;
-    if (n_rb > (((int64_t)1 << 31) - 8) / n_cs) return hipErrorNotSupported;
+    if (n_rb > (((int64_t)1 << 24) - 8) / n_cs) return hipErrorNotSupported;
     const int64_t n_tiles = n_rb * n_cs, per_xcd = (n_tiles + 7) / 8;
     hipLaunchKernelGGL((dequant128_col_kernel<FMT, DT>), dim3((unsigned)(per_xcd * 8)), dim3(256), 0, st, elems, scales, shift, rows, cols, ld, n_rb, n_tiles, per_xcd, dst);
     return hipGetLastError();

@@ -8,7 +8,7 @@ template <int FA, int FB, int CDT, bool ROWS_B, int MB, int NB, int WM, int WN>
 static hipError_t launch_tiles(const Gemm128 &g, hipStream_t st)
 {
     const int64_t tm = (g.M + 16 * MB * WM - 1) / (16 * MB * WM), tn = (g.N + 16 * NB * WN - 1) / (16 * NB * WN);
-    if (tm > ((int64_t)1 << 30) / tn) return hipErrorNotSupported;
+    if (tm > ((int64_t)1 << 22) / tn) return hipErrorNotSupported;     // (the runtime counts a grid's threads in 32 bits)
     const Bands order = bands(tm, tn, 6);
     hipLaunchKernelGGL((gemm128_kernel<FA, FB, CDT, ROWS_B, MB, NB, WM, WN>), dim3(8 * order.per_xcd), dim3(64 * WM * WN), 0, st, g, order);
     return hipGetLastError();
@@ -18,7 +18,7 @@ template <int FA, int FB, int CDT, bool ROWS_B, int MB, int NB, int AHEAD>
 static hipError_t launch_few(const Gemm128 &g, hipStream_t st)
 {
     const int64_t gx = (g.N + 16 * NB - 1) / (16 * NB), gy = (g.M + 16 * MB - 1) / (16 * MB);
-    if (gx > ((int64_t)1 << 31) - 1 || gy > 65535) return hipErrorNotSupported;
+    if (gx >= (int64_t)1 << 23) return hipErrorNotSupported;           // (the runtime counts a grid's threads in 32 bits; M is at most 64)
     hipLaunchKernelGGL((gemm128_few_kernel<FA, FB, CDT, ROWS_B, MB, NB, AHEAD>), dim3((unsigned)gx, (unsigned)gy), dim3(512), 0, st, g);
     return hipGetLastError();
 }

@@ -270,7 +270,7 @@ static hipError_t launch_tile(const Gemm128 &g, hipStream_t st)
 {
     constexpr int BM = 16 * MB * WM, BN = 16 * NB * WN;
     const int64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN;
-    if (tm > ((int64_t)1 << 30) / tn) return hipErrorNotSupported;
+    if (tm > ((int64_t)1 << 22) / tn) return hipErrorNotSupported;     // (the runtime counts a grid's threads in 32 bits)
     const Bands order = bands(tm, tn, BM == 256 ? 4 : 6);
     hipLaunchKernelGGL((gemm128_tile_kernel<FA, FB, CDT, ROWS_B, MB, NB, WM, WN, KS>), dim3(8 * order.per_xcd), dim3(512), 0, st, g, order);
     return hipGetLastError();

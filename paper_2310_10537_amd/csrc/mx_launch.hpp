@@ -116,8 +116,8 @@ hipError_t launch_gemm_tiled_mx(int64_t M, int64_t N, int64_t K, const uint8_t *
                                 const uint8_t *Be, const uint8_t *Bs, int fmtB, uint8_t *Ce, uint8_t *Cs, int fmtC, int rndC,
                                 hipStream_t st);
 
-// 8-bit formats with a Float32 scale for each block of 128 along the lines, or each 128 x 128 tile; hipErrorNotSupported beyond 2^31 - 8 tiles,
-// or lines of more than about 2^33 elements
+// 8-bit formats with a Float32 scale for each block of 128 along the lines, or each 128 x 128 tile; hipErrorNotSupported beyond about 2^24 tiles
+// (of 128 x 64 where the transpose is dequantized), or lines of more than about 2^33 elements
 hipError_t launch_cast_b128(const void *src, int src_dt, int64_t rows, int64_t cols, int64_t ld, int axis, bool tile, int fmt, uint8_t *elems,
                             float *scales, hipStream_t st);
 hipError_t launch_dequant_b128(const uint8_t *elems, const float *scales, int fmt, int64_t rows, int64_t cols, int axis, bool tile, void *dst,

@@ -228,6 +228,10 @@ struct NormArgs {
     int64_t rows, cols, ldx, ldr, ldh, ldy;
     float eps;
     int w_dt, rnd, nvec;
+    int64_t row0;         // first row of a launch
 };
+
+// rows that one launch may have with `threads` threads for each: the runtime counts a grid's threads in 32 bits
+inline int64_t rows_per_launch(int threads) { return (((int64_t)1 << 32) - 1) / threads / 4 * 4; }
 
 }  // namespace mx

@@ -19,6 +19,7 @@ struct NormBwdArgs {
     float *partial;       // [lines][cols], or nullptr: no dweight
     int64_t rows, cols, lddy, ldh, lddh, lddx;
     int w_dt;
+    int64_t row0;         // (norm_bwd_long_kernel) first row of a launch
 };
 
 template <int DT> struct Vec8 { uint32_t d[DT == DT_BF16 ? 4 : 8]; };
@@ -197,7 +198,7 @@ template <int DT>
 __global__ __launch_bounds__(256) void norm_bwd_long_kernel(NormBwdArgs a)
 {
     __shared__ float lds[4];
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
     const float rstd = a.rstd[row];
     float sum = 0.0f;
     for (int64_t col = threadIdx.x * 8; col < a.cols; col += 2048) {
@@ -273,10 +274,14 @@ static hipError_t launch_norm_bwd_t(const NormBwdArgs &a, int lines, float *dwei
 {
     const dim3 b(256), g((unsigned)lines);
     if (a.cols > NORM_BWD_COLS) {
-        if (a.rows > ((int64_t)1 << 31) - 1 || a.cols > ((int64_t)1 << 36)) return hipErrorNotSupported;
         if (a.partial)                                // first: dx may take the place of dy
             hipLaunchKernelGGL((norm_bwd_long_weight_kernel<DT>), dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)lines), b, 0, st, a);
-        hipLaunchKernelGGL((norm_bwd_long_kernel<DT>), dim3((unsigned)a.rows), b, 0, st, a);
+        const int64_t most = rows_per_launch(256);
+        for (int64_t r0 = 0; r0 < a.rows; r0 += most) {
+            NormBwdArgs part = a;
+            part.row0 = r0;
+            hipLaunchKernelGGL((norm_bwd_long_kernel<DT>), dim3((unsigned)(a.rows - r0 < most ? a.rows - r0 : most)), b, 0, st, part);
+        }
     } else {
         const dim3 threads(norm_bwd_threads(a.cols));
         if (a.cols <= 512) hipLaunchKernelGGL((norm_bwd_kernel<DT, 1, true>), g, threads, 0, st, a);
@@ -291,7 +296,7 @@ static hipError_t launch_norm_bwd_t(const NormBwdArgs &a, int lines, float *dwei
 hipError_t launch_norm_bwd(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *weight, int w_dt, const float *rstd, const void *dh, int64_t lddh,
                            int dt, int64_t rows, int64_t cols, void *dx, int64_t lddx, float *dweight, hipStream_t st)
 {
-    NormBwdArgs a = {dy, h, weight, dh, rstd, dx, nullptr, rows, cols, lddy, ldh, lddh, lddx, w_dt};
+    NormBwdArgs a = {dy, h, weight, dh, rstd, dx, nullptr, rows, cols, lddy, ldh, lddh, lddx, w_dt, 0};
     if (rows == 0) {                                  // an empty sum
         hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, st, a.partial, 0, cols, dweight);
         return hipGetLastError();

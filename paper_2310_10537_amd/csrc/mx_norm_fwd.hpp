@@ -55,7 +55,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a)
     norm_modes<OUT>();
     __shared__ float lds[16];
     const int nt = WAVE ? 64 : (int)blockDim.x, t = WAVE ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+    const int64_t row = a.row0 + (WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x);
     if (WAVE && row >= a.rows) return;                // (a whole wave; the kernel has no barrier then)
     float h[VPT][8], sum = 0.0f;
 #pragma unroll
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
 {
     norm_modes<OUT>();
     __shared__ float lds[16];
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
     float sum = 0.0f;
     for (int vec = threadIdx.x; vec < a.nvec; vec += 1024) {
         const int64_t col = (int64_t)vec * 8;
@@ -113,10 +113,18 @@ template <int OUT, int DT>
 static hipError_t launch_norm_t(const NormArgs &a, hipStream_t st)
 {
     const int threads = a.nvec <= 1024 ? (a.nvec + 63) / 64 * 64 : a.nvec <= 2048 ? (a.nvec + 127) / 128 * 64 : 1024;
-    if (a.nvec <= 64) hipLaunchKernelGGL((norm_kernel<OUT, DT, 1, true>), dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, st, a);
-    else if (a.nvec <= 1024) hipLaunchKernelGGL((norm_kernel<OUT, DT, 1, false>), dim3((unsigned)a.rows), dim3(threads), 0, st, a);
-    else if (a.nvec <= 2048) hipLaunchKernelGGL((norm_kernel<OUT, DT, 2, false>), dim3((unsigned)a.rows), dim3(threads), 0, st, a);
-    else hipLaunchKernelGGL((norm_long_kernel<OUT, DT>), dim3((unsigned)a.rows), dim3(threads), 0, st, a);
+    const bool waves = a.nvec <= 64;                  // four rows a work-group of 256
+    const int64_t most = rows_per_launch(threads);
+    for (int64_t r0 = 0; r0 < a.rows; r0 += most) {
+        NormArgs b = a;
+        b.row0 = r0;
+        const int64_t n = a.rows - r0 < most ? a.rows - r0 : most;
+        const dim3 grid((unsigned)(waves ? (n + 3) / 4 : n));
+        if (waves) hipLaunchKernelGGL((norm_kernel<OUT, DT, 1, true>), grid, dim3(256), 0, st, b);
+        else if (a.nvec <= 1024) hipLaunchKernelGGL((norm_kernel<OUT, DT, 1, false>), grid, dim3(threads), 0, st, b);
+        else if (a.nvec <= 2048) hipLaunchKernelGGL((norm_kernel<OUT, DT, 2, false>), grid, dim3(threads), 0, st, b);
+        else hipLaunchKernelGGL((norm_long_kernel<OUT, DT>), grid, dim3(threads), 0, st, b);
+    }
     return hipGetLastError();
 }
 
