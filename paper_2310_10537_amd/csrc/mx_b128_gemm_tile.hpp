@@ -271,7 +271,9 @@ static hipError_t launch_tile(const Gemm128 &g, hipStream_t st)
     constexpr int BM = 16 * MB * WM, BN = 16 * NB * WN;
     const int64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN;
     if (tm > ((int64_t)1 << 22) / tn) return hipErrorNotSupported;     // (the runtime counts a grid's threads in 32 bits)
-    const Bands order = bands(tm, tn, BM == 256 ? 4 : 6);
+    // a work-group of 256 x 256 has a compute unit to itself, so 32 of them run on an XCD: 5 rows by 6 to 7 columns fetch least (8192 x 11008 x 4096: 2.21
+    // PFLOP/s in bands of 5, 2.20 of 6, 2.14 of 4; 16384 x 8192 x 2048: 2.13, 2.09, 2.00)
+    const Bands order = bands(tm, tn, BM == 256 && BN == 256 ? 5 : 6);
     hipLaunchKernelGGL((gemm128_tile_kernel<FA, FB, CDT, ROWS_B, MB, NB, WM, WN, KS>), dim3(8 * order.per_xcd), dim3(512), 0, st, g, order);
     return hipGetLastError();
 }
