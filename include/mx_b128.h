@@ -44,7 +44,9 @@ size_t mx_b128_scale_count(int64_t rows, int64_t cols, int axis, int tile);
  *     elem   = the element nearest to the Float32 product v * factor, ties to
  *              even; beyond fmax, fmax; a NaN gives NaN, an infinity NaN (E4M3)
  *              or infinity (E5M2).
- * (The cut makes v * factor exact for bf16 v.  A block of zeros gets scale 2^-126.)
+ * (The cut makes v * factor exact for bf16 v.  A block of zeros gets scale 2^-126.  It
+ * may raise the scale by 2^-15 of itself: a Float32 v that close to the type's largest
+ * number can stand for infinity.)
  * Outputs are 16-byte aligned, of the sizes above.
  * MX_ERR_UNSUPPORTED: more than about 2^24 tiles of 128 x 128 (with axis 0 or tile
  * 1), or rows longer than about 2^33 elements (else).

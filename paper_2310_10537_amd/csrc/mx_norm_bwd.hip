@@ -168,7 +168,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_bwd_kernel(NormBwdArgs
 }
 
 // dweight[c] = partial[0][c] + partial[1][c] + ..., 16 columns and 64 runs of lines a work-group
-__global__ __launch_bounds__(1024) void norm_bwd_weight_kernel(const float *__restrict__ partial, int lines, int64_t cols, float *__restrict__ dweight)
+__global__ __launch_bounds__(1024) void norm_bwd_weight_kernel(const float *__restrict__ partial, int lines, int64_t pitch, int64_t cols, float *__restrict__ dweight)
 {
     __shared__ float part[64][17];
     const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
@@ -179,11 +179,11 @@ __global__ __launch_bounds__(1024) void norm_bwd_weight_kernel(const float *__re
         for (; l + 448 < lines; l += 512) {
             float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) v[j] = partial[(int64_t)(l + 64 * j) * cols + col];
+            for (int j = 0; j < 8; j++) v[j] = partial[(int64_t)(l + 64 * j) * pitch + col];
 #pragma unroll
             for (int j = 0; j < 8; j++) sum += v[j];
         }
-        for (; l < lines; l += 64) sum += partial[(int64_t)l * cols + col];
+        for (; l < lines; l += 64) sum += partial[(int64_t)l * pitch + col];
     }
     part[g][c] = sum;
     __syncthreads();
@@ -269,6 +269,15 @@ size_t norm_bwd_workspace(int64_t rows, int64_t cols)
     return ((size_t)norm_bwd_lines(rows, cols) * (size_t)cols * 4 + 255) & ~(size_t)255;
 }
 
+static void launch_norm_bwd_weight(const float *partial, int lines, int64_t cols, float *dweight, hipStream_t st)
+{
+    constexpr int64_t MOST = (int64_t)1 << 25;        // columns a launch: the runtime counts a grid's threads in 32 bits
+    for (int64_t c0 = 0; c0 < cols; c0 += MOST) {
+        const int64_t n = cols - c0 < MOST ? cols - c0 : MOST;
+        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((n + 15) / 16)), dim3(1024), 0, st, partial ? partial + c0 : nullptr, lines, cols, n, dweight + c0);
+    }
+}
+
 template <int DT>
 static hipError_t launch_norm_bwd_t(const NormBwdArgs &a, int lines, float *dweight, hipStream_t st)
 {
@@ -288,8 +297,7 @@ static hipError_t launch_norm_bwd_t(const NormBwdArgs &a, int lines, float *dwei
         else if (a.cols <= 8192) hipLaunchKernelGGL((norm_bwd_kernel<DT, 1, false>), g, threads, 0, st, a);
         else hipLaunchKernelGGL((norm_bwd_kernel<DT, 2, false>), g, threads, 0, st, a);
     }
-    if (a.partial)
-        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((a.cols + 15) / 16)), dim3(1024), 0, st, a.partial, lines, a.cols, dweight);
+    if (a.partial) launch_norm_bwd_weight(a.partial, lines, a.cols, dweight, st);
     return hipGetLastError();
 }
 
@@ -298,7 +306,7 @@ hipError_t launch_norm_bwd(const void *dy, int64_t lddy, const void *h, int64_t 
 {
     NormBwdArgs a = {dy, h, weight, dh, rstd, dx, nullptr, rows, cols, lddy, ldh, lddh, lddx, w_dt, 0};
     if (rows == 0) {                                  // an empty sum
-        hipLaunchKernelGGL(norm_bwd_weight_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, st, a.partial, 0, cols, dweight);
+        launch_norm_bwd_weight(nullptr, 0, cols, dweight, st);
         return hipGetLastError();
     }
     uint8_t *ws = nullptr;

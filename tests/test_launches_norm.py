@@ -107,3 +107,11 @@ def test_gradients(trace, norm_calls):
     assert names(one(trace, *norm_calls(0, 64))) == [("norm_bwd_weight_kernel",)]
     seen = one(trace, *norm_calls((1 << 24) + 5, 16392, dw=0))
     assert len(seen) == 2 and grids_fit(seen) and sum(k[2][0] for k in seen) == (1 << 24) + 5
+
+
+def test_gradients_of_very_wide_rows(trace, norm_calls):
+    for cols in ((1 << 26) - 8, 1 << 26, (1 << 30) + 8):
+        for rows in (0, 3):
+            seen = one(trace, *norm_calls(rows, cols))
+            assert grids_fit(seen)
+            assert sum(k[2][0] for k in seen if k[0] == "norm_bwd_weight_kernel") * 16 >= cols
