@@ -48,8 +48,8 @@ size_t mx_b128_scale_count(int64_t rows, int64_t cols, int axis, int tile);
  * may raise the scale by 2^-15 of itself: a Float32 v that close to the type's largest
  * number can stand for infinity.)
  * Outputs are 16-byte aligned, of the sizes above.
- * MX_ERR_UNSUPPORTED: more than about 2^24 tiles of 128 x 128 (with axis 0 or tile
- * 1), or rows longer than about 2^33 elements (else).
+ * MX_ERR_UNSUPPORTED: more than about 2^24 tiles of 128 x 128 (with axis 0 or tile 1;
+ * of 128 x 64 with axis 0, tile 0 and bf16), or rows longer than about 2^33 elements (else).
  */
 int mx_quantize_b128(const void *src, mx_dtype_t src_dt, int64_t rows, int64_t cols,
                      int64_t ld, int axis, int tile, mx_format_t fmt,
@@ -58,7 +58,7 @@ int mx_quantize_b128(const void *src, mx_dtype_t src_dt, int64_t rows, int64_t c
 /* elems * scales, rounded to Float32 and from there to dst_dt, into the row-major
  * dst [rows, cols] with leading dimension ld; arguments as mx_dequantize.  The fill
  * of a partial last block is skipped.  MX_ERR_UNSUPPORTED: as above, with axis 0
- * more than about 2^24 tiles of 128 x 64. */
+ * more than about 2^24 tiles of 128 x 64 whatever the type. */
 int mx_dequantize_b128(const void *elems, const float *scales, mx_format_t fmt,
                        int64_t rows, int64_t cols, int axis, int tile,
                        void *dst, mx_dtype_t dst_dt, int64_t ld, void *hip_stream);
