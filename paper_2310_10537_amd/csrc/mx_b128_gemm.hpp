@@ -167,12 +167,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm128_kernel(Gemm128 g, Ban
 #pragma unroll
         for (int j = 0; j < NJA; j++) {
             const uint8_t *p = pA[j] + (int64_t)t * 128;
-            asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds0 + buf * STAGE + j * NW * 1024) : "m0", "memory");
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds0 + buf * STAGE + j * NW * 1024) : "m0", "memory");
         }
 #pragma unroll
         for (int j = 0; j < NJB; j++) {
             const uint8_t *p = pB[j] + (int64_t)t * 128;
-            asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds0 + buf * STAGE + A_BYTES + j * NW * 1024) : "m0", "memory");
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds0 + buf * STAGE + A_BYTES + j * NW * 1024) : "m0", "memory");
         }
     };
     // ---- scales of blocks 4G .. 4G + 3: thread r those of row r of A, then of B

@@ -31,6 +31,16 @@ __device__ __forceinline__ void block_product_at(v4f_t &p, const v8i_t &b, const
     asm volatile("v_mfma_f32_16x16x128_f8f6f4 %0, %1, %2, 0 cbsz:%3 blgp:%4" : "=&v"(p) : "v"(b), "v"(a), "n"(HB), "n"(HA) : "memory");
 }
 
+// ... with a direct load of 1 KB behind it, from base + o (a lane's bytes) to LDS byte dst + AT.  A write to M0 wants an instruction before its reader:
+// the product stands there (2 % faster over eleven large products than with one of its own).
+template <int FA, int FB, int AT>
+__device__ __forceinline__ void block_product_and_load_at(v4f_t &p, const v8i_t &b, const v8i_t &a, uint32_t o, const uint8_t *base, uint32_t dst)
+{
+    constexpr int HA = hw_fmt(FA), HB = hw_fmt(FB);
+    asm volatile("s_add_u32 m0, %7, %8\n\tv_mfma_f32_16x16x128_f8f6f4 %0, %1, %2, 0 cbsz:%3 blgp:%4\n\tglobal_load_lds_dwordx4 %5, %6"
+                 : "=&v"(p) : "v"(b), "v"(a), "n"(HB), "n"(HA), "v"(o), "s"(base), "s"(dst), "n"(AT) : "m0", "scc", "memory");
+}
+
 // a pointer that every lane of a wave has the same value of, in scalar registers
 __device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
 {
@@ -79,6 +89,7 @@ __global__ __launch_bounds__(512, 2) void gemm128_tile_kernel(Gemm128 g, Bands o
     // ---- staging: load j of wave w fills rows 8 NW j + 8 w .. + 7 of the tile, lane l slot l % 8 of row l / 8.  Offsets are 32 bits from the
     // tile's first row (K below 2^24); rows beyond the matrix read its last one.
     constexpr int NJA = BM / 8 / NW, NJB = BN / 8 / NW, NJ = NJA + NJB;
+    static_assert(NJA * NW * 1024 == A_BYTES, "B's stage lies behind A's");
     typedef __attribute__((address_space(3))) void lds_ptr_t;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t *)lds) + wave * 1024;
     const int s_r = wave * 8 + (lane >> 3);
@@ -86,14 +97,16 @@ __global__ __launch_bounds__(512, 2) void gemm128_tile_kernel(Gemm128 g, Bands o
     const uint32_t ofs = (uint32_t)s_r * K32 + chunk;
     const uint32_t lastA = (uint32_t)(rows_a - 1) * K32 + chunk, lastB = (uint32_t)(rows_b - 1) * K32 + chunk;
     const uint8_t *const gA = uniform(g.Ae + m0 * g.K + (int64_t)t_first * 128), *const gB = uniform(g.Be + n0 * g.K + (int64_t)t_first * 128);
-    auto load_one = [&](auto number, const uint8_t *atA, const uint8_t *atB, uint32_t dst) __attribute__((always_inline)) {   // one direct load of a stage: A's, then B's
+    auto source = [&](auto number) __attribute__((always_inline)) {               // offset of direct load k of a stage: A's, then B's (to LDS byte 1024 k NW)
+        constexpr int k = decltype(number)::value, j = k < NJA ? k : k - NJA;
+        const uint32_t o = ofs + (uint32_t)(8 * NW * j) * K32, last = k < NJA ? lastA : lastB;
+        return o < last ? o : last;
+    };
+    auto load_one = [&](auto number, const uint8_t *atA, const uint8_t *atB, uint32_t dst) __attribute__((always_inline)) {
         constexpr int k = decltype(number)::value;
-        constexpr bool of_a = k < NJA;
-        constexpr int j = of_a ? k : k - NJA;
-        uint32_t o = ofs + (uint32_t)(8 * NW * j) * K32;
-        const uint32_t last = of_a ? lastA : lastB;
-        o = o < last ? o : last;
-        asm volatile("s_add_u32 m0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(o), "s"(of_a ? atA : atB), "s"(dst), "n"((of_a ? 0 : A_BYTES) + j * NW * 1024) : "m0", "scc", "memory");
+        const uint32_t o = source(number);
+        const uint8_t *const base = k < NJA ? atA : atB;
+        asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(o), "s"(base), "s"(dst), "n"(k * NW * 1024) : "m0", "scc", "memory");
     };
     // ---- scales, four blocks at a time: those of blocks first(G) .. + 3, G = 0, 1, ...; the last group of a row is its last four
     auto first = [&](int G) { return 4 * G + 4 <= T ? 4 * G : T - 4; };
@@ -155,15 +168,16 @@ __global__ __launch_bounds__(512, 2) void gemm128_tile_kernel(Gemm128 g, Bands o
         for (int e = 0; e < 4; e++) acc[x][y][e] = fmaf(p[k & 3][e], ROWS_B ? f[x] * bs[y & 1][e] : f[x], acc[x][y][e]);
         asm volatile("" : "+v"(acc[x][y]));           // (here, not where the sum is wanted: the ring's place is wanted before)
     };
-    auto tile = [&](auto number, const float *sc, const float (&f)[MB], auto also, auto beside) __attribute__((always_inline)) {
+    auto tile = [&](auto number, const float *sc, const float (&f)[MB], auto also, auto beside, auto product) __attribute__((always_inline)) {
         constexpr int k = decltype(number)::value, x = k % MB, y = k / MB, back = (k + NT - 3) % NT;
         if constexpr (decltype(also)::value) asm volatile("" : "+v"(p[back & 3]));
-        block_product_at<FA, FB>(p[k & 3], b[y % RING], a[x]);
+        product(number, p[k & 3], b[y % RING], a[x]);
         beside(number);
         if constexpr (decltype(also)::value) scale_tile(std::integral_constant<int, back>(), f);
         if constexpr (ROWS_B && x == 2) bs[(y + 1) & 1] = *reinterpret_cast<const v4f_t *>(sc + 16 * ((y + 1) % NB));
         __builtin_amdgcn_sched_barrier(0);
     };
+    auto alone = [](auto, v4f_t &to, const v8i_t &fb, const v8i_t &fa) __attribute__((always_inline)) { block_product_at<FA, FB>(to, fb, fa); };
     constexpr std::true_type with;
     constexpr std::false_type without;
     static_assert(NT % 4 == 0, "the ring's places repeat from step to step");
@@ -194,9 +208,9 @@ __global__ __launch_bounds__(512, 2) void gemm128_tile_kernel(Gemm128 g, Bands o
             if constexpr (RING < NB && x == MB - 1) b[y % RING] = frag(cur, rb0, y + RING);
         };
     };
-    each<3>([&](auto k) { tile(k, scale_row(0) + sb0, s, without, front(0)); });
+    each<3>([&](auto k) { tile(k, scale_row(0) + sb0, s, without, front(0), alone); });
     asm volatile("s_nop 15" : "+v"(p[0]));            // (nothing stands between these three and the first multiply-adds)
-    each<FRONT - 3>([&](auto d) { tile(std::integral_constant<int, 3 + decltype(d)::value>(), scale_row(0) + sb0, s, with, front(0)); });
+    each<FRONT - 3>([&](auto d) { tile(std::integral_constant<int, 3 + decltype(d)::value>(), scale_row(0) + sb0, s, with, front(0), alone); });
     for (int t = 0; t + 1 < T; t++) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if ((t & 3) == 2 && t + 2 < T) park_scales((t >> 2) + 1);
@@ -210,32 +224,36 @@ __global__ __launch_bounds__(512, 2) void gemm128_tile_kernel(Gemm128 g, Bands o
         float sb1 = 1.0f;
         auto fill = [&](auto number) __attribute__((always_inline)) {
             constexpr int k = decltype(number)::value, x = k % MB, y = k / MB, d = k - FRONT;
-            if constexpr (d < NJ) load_one(std::integral_constant<int, d>(), atA, atB, dst);
             if constexpr (RING == NB && (d == 2 || d == 5)) b[d / 3] = frag(nxt, rb0, d / 3);     // the first two columns' fragments fell free before
             if constexpr (x == MB - 1) b[y % RING] = frag(nxt, rb0, y % RING);
             if constexpr (y == NB - 1) a[x] = frag(nxt, ra0, x);
             if constexpr (y == NB - 1) sn[x] = sc1[sa0 + 16 * x];
             if constexpr (!ROWS_B && k == NT - MB) sb1 = sc1[sb_tile];
         };
+        auto and_load = [&](auto number, v4f_t &to, const v8i_t &fb, const v8i_t &fa) __attribute__((always_inline)) {
+            constexpr int d = decltype(number)::value - FRONT;
+            if constexpr (d < NJ) block_product_and_load_at<FA, FB, d * NW * 1024>(to, fb, fa, source(std::integral_constant<int, d>()), d < NJA ? atA : atB, dst);
+            else alone(number, to, fb, fa);
+        };
         each<NT - FRONT>([&](auto d) {
             constexpr int k = FRONT + decltype(d)::value;
             const std::integral_constant<int, k> number;
             const float *const of = ROWS_B && k / MB == NB - 1 ? sc1 + sb0 : sc;  // (the scales fetched ahead in the last column are the next step's)
-            tile(number, of, s, with, fill);
+            tile(number, of, s, with, fill, and_load);
         });
         each<FRONT>([&](auto k) {
             if constexpr (!ROWS_B && k() < MB) {
                 constexpr int x = decltype(k)::value;
-                tile(k, sc1 + sb0, x < 3 ? s : sn, with, [&](auto n) { sn[x] *= sb1; front(nxt)(n); });
+                tile(k, sc1 + sb0, x < 3 ? s : sn, with, [&](auto n) { sn[x] *= sb1; front(nxt)(n); }, alone);
             } else {
-                if constexpr (k() < 3) tile(k, sc1 + sb0, s, with, front(nxt));
-                else tile(k, sc1 + sb0, sn, with, front(nxt));
+                if constexpr (k() < 3) tile(k, sc1 + sb0, s, with, front(nxt), alone);
+                else tile(k, sc1 + sb0, sn, with, front(nxt), alone);
             }
         });
 #pragma unroll
         for (int x = 0; x < MB; x++) s[x] = sn[x];
     }
-    each<NT - FRONT>([&](auto d) { tile(std::integral_constant<int, FRONT + decltype(d)::value>(), scale_row(T - 1) + sb0, s, with, [](auto) {}); });
+    each<NT - FRONT>([&](auto d) { tile(std::integral_constant<int, FRONT + decltype(d)::value>(), scale_row(T - 1) + sb0, s, with, [](auto) {}, alone); });
     each<3>([&](auto k) {
         asm volatile("s_nop 3" : "+v"(p[(NT - 3 + k()) & 3]));
         scale_tile(std::integral_constant<int, NT - 3 + k()>(), s);
