@@ -1,5 +1,6 @@
 // Values of 8-bit floating point with a Float32 scale for each block of 128 or each 128 x 128 tile:
 // v = fl(code * scale), rounded once more for a bf16 result.  Bound by memory: 1 byte + 4/128 read, 2 or 4 written.
+// 8192 x 8192 to bf16 34.9 us (5.8 TB/s), of the transpose's codes 43.9 (4.6); to Float32 54.6 (6.2).
 //
 //   dequant128_row_kernel   codes in the order of the result.  A lane takes as many codes as make one 16-byte store: 8 (16 lanes a block) or, of a
 //       Float32 result, 4; four loads in flight.  (Two 16-byte stores 32 bytes apart leave every line half written: 4.4 TB/s, not 5.9.)

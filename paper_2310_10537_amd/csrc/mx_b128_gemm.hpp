@@ -5,8 +5,7 @@
 // The 16 x 16 x 128 matrix instruction adds exactly the products of one block, from zero, so a scale meets its partial sum in one Float32
 // multiply-add per entry and block.  That vector work decides the layout: accumulators have to be in the vector
 // registers (the instructions that scale them cannot reach the accumulation registers), 256 of them a lane at most, so
-// a 256 x 256 tile takes eight waves of 64 x 128 entries (128 accumulators a lane), two on each SIMD: while one wave's
-// matrix instructions run (32 clocks each) the other's multiply-adds (4 of 4 clocks per instruction) fill the vector pipe.
+// a 256 x 256 tile takes eight waves of 64 x 128 entries (128 accumulators a lane), two on each SIMD (mx_b128_gemm_tile.hpp).
 // The B fragment goes first: a lane (i, q) then holds row i of A and four consecutive columns 4q .. 4q + 3, so the scale of A is one
 // number a lane and 16-row block, and where B has a scale for 128 columns that one is the same for the whole wave (its columns lie in one
 // block of 128): one product a lane, block and 16 rows, all else is multiply-adds.  With a scale a column of B four products and four multiply-adds.

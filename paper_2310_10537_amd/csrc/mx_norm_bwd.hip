@@ -1,7 +1,8 @@
 // Gradients of the RMS norm y = h rstd w (the cast behind it passes its gradient through), with g = dy w and xhat = h rstd:
 //     dx = rstd (g - xhat mean(g xhat)) + dh,        dweight = sum over rows of dy xhat.
 // dx is the gradient of x and of the residual alike; dh is the gradient that reaches h past the layer.
-// Bound by memory: dy, h (and dh) read and dx written, once; everything else is small.
+// Bound by memory: dy, h (and dh) read and dx written, once; everything else is small.  16384 x 2048 bf16 with a dh 49.6 us with dweight (5.4 TB/s), of
+// which the lines of partial sums take 4; 2048 x 16384 63 (4.3 TB/s: two vectors a thread, nothing on its way during a row's sum).
 //
 // norm_bwd_kernel: a number of work-groups that the shape fixes walks the rows; a row lies in registers, a vector of eight columns a thread
 // (two beyond 8192 columns; a wave a row up to 512), the weight is kept from row to row, and every thread adds up its own columns'
