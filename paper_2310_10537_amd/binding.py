@@ -436,42 +436,48 @@ def mx_dequantize_3d(elems, scales, fmt, shape, axis, keep_order=False, dtype=to
 BLOCK128 = 128
 
 
-def _call(device, stream, fn, *args):
+def _call(index, stream, fn, *args):
     """A library function on the device of a call's tensors and on the given stream, else torch's current one of that device."""
-    index = device.index
     raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         status = fn(*args, raw)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             status = fn(*args, raw)
     if status != MX_OK:
         _check(status)
 
 
-def _rows(t, name, like=None):
-    """Pitch (elements) of a 2-D float32 / bfloat16 device tensor whose rows are contiguous; `like`: it has that tensor's shape, type and device."""
-    if not t.is_cuda:
+def _where(t, name):
+    """Index of the device that a tensor lives on."""
+    index = t.get_device()
+    if index < 0 or not t.is_cuda:
         raise ValueError(f"{name} must live in device memory")
-    shape = t.shape
-    if len(shape) != 2:
-        raise ValueError(f"{name} must be a matrix with contiguous rows")
+    return index
+
+
+def _rows(t, name, shape, dtype, index):
+    """Pitch (elements) of a matrix of this shape, type (float32 / bfloat16) and device whose rows are contiguous."""
+    if t.dtype != dtype or t.shape != shape or t.get_device() != index or len(shape) != 2:
+        raise ValueError(f"{name} must be a matrix {list(shape)} of {dtype} on device {index}")
     pitch, step = t.stride()
     if step != 1 and shape[1] > 1:
-        raise ValueError(f"{name} must be a matrix with contiguous rows")
-    if like is not None and (shape != like.shape or t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{name} must have the shape {tuple(like.shape)}, type and device of the tensor it goes with")
+        raise ValueError(f"{name} must have contiguous rows")
     if shape[0] > 1:
         return pitch
-    per16 = 16 // t.element_size()
+    per16 = 16 // dtype.itemsize
     return -(-shape[1] // per16) * per16              # one row: its pitch is never used, but has to be a possible one
 
 
-def _flat(t, name, shape, dtype, device):
-    """A contiguous tensor of exactly this shape and type."""
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {device}")
+def _flat(t, name, shape, dtype, index):
+    """A contiguous tensor of exactly this shape, type and device."""
+    if t.dtype != dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on device {index}")
     return t
+
+
+def _made(shape, dtype, index):
+    return torch.empty(shape, dtype=dtype, device=index)
 
 
 def _b128_shapes(rows, cols, axis, tile):
@@ -483,62 +489,61 @@ def _b128_shapes(rows, cols, axis, tile):
 def mx_quantize_b128(src, axis, fmt, tile=False, elems_out=None, scales_out=None, stream=None):
     """src: 2-D device tensor (float32 / bfloat16, rows contiguous).  Returns (elems uint8 [lines, 128 blocks],
     scales float32 [lines, blocks], or [lines / 128, blocks] with tile): blocks of 128 along `axis`, or 128 x 128 tiles."""
-    ld = _rows(src, "src")
-    dt = _dt(src)
-    rows, cols = src.shape
+    index, shape, dt = _where(src, "src"), src.shape, _dt(src)
+    ld = _rows(src, "src", shape, src.dtype, index)
+    rows, cols = shape
     shape_e, shape_s = _b128_shapes(rows, cols, axis, tile)
-    elems = torch.empty(shape_e, dtype=torch.uint8, device=src.device) if elems_out is None else _flat(elems_out, "elems_out", shape_e, torch.uint8, src.device)
-    scales = torch.empty(shape_s, dtype=torch.float32, device=src.device) if scales_out is None else _flat(scales_out, "scales_out", shape_s, torch.float32, src.device)
-    _call(src.device, stream, lib().mx_quantize_b128, src.data_ptr(), dt, rows, cols, ld, axis, 1 if tile else 0, fmt, elems.data_ptr(), scales.data_ptr())
+    elems = _made(shape_e, torch.uint8, index) if elems_out is None else _flat(elems_out, "elems_out", shape_e, torch.uint8, index)
+    scales = _made(shape_s, torch.float32, index) if scales_out is None else _flat(scales_out, "scales_out", shape_s, torch.float32, index)
+    _call(index, stream, lib().mx_quantize_b128, src.data_ptr(), dt, rows, cols, ld, axis, 1 if tile else 0, fmt, elems.data_ptr(), scales.data_ptr())
     return elems, scales
 
 
 def mx_dequantize_b128(elems, scales, fmt, rows, cols, axis, tile=False, dtype=torch.float32, out=None, stream=None):
     """Returns the row-major [rows, cols] tensor of elems * scales (axis and tile as cast)."""
-    _dev(elems, "elems")
+    index = _where(elems, "elems")
     shape_e, shape_s = _b128_shapes(rows, cols, axis, tile)
-    _flat(elems, "elems", shape_e, torch.uint8, elems.device)
-    _flat(scales, "scales", shape_s, torch.float32, elems.device)
+    _flat(elems, "elems", shape_e, torch.uint8, index)
+    _flat(scales, "scales", shape_s, torch.float32, index)
     if out is None:
-        out = _empty_rows(rows, cols, dtype, elems.device)
-    elif tuple(out.shape) != (rows, cols) or out.device != elems.device:
-        raise ValueError(f"out must be a [{rows}, {cols}] tensor on {elems.device}")
-    ld = _rows(out, "out")
-    _call(elems.device, stream, lib().mx_dequantize_b128, elems.data_ptr(), scales.data_ptr(), fmt, rows, cols, axis, 1 if tile else 0, out.data_ptr(), _dt(out), ld)
+        out = _empty_rows(rows, cols, dtype, index)
+    dt = _dt(out)
+    ld = _rows(out, "out", (rows, cols), out.dtype, index)
+    _call(index, stream, lib().mx_dequantize_b128, elems.data_ptr(), scales.data_ptr(), fmt, rows, cols, axis, 1 if tile else 0, out.data_ptr(), dt, ld)
     return out
 
 
-def _empty_rows(rows, cols, dtype, device):
+def _empty_rows(rows, cols, dtype, index):
     """A matrix whose rows start at multiples of 16 bytes."""
     per16 = 8 if dtype == torch.bfloat16 else 4
     if cols % per16 == 0 or rows <= 1:
-        return torch.empty((rows, cols), dtype=dtype, device=device)
-    return torch.empty((rows, -(-cols // per16) * per16), dtype=dtype, device=device)[:, :cols]
+        return _made((rows, cols), dtype, index)
+    return _made((rows, -(-cols // per16) * per16), dtype, index)[:, :cols]
 
 
-def _b128_operand(elems, scales, name, K):
+def _b128_operand(elems, scales, name, K, index):
     """(lines, whether the scales are those of 128 x 128 tiles) of a product's operand."""
-    _dev(elems, name + "_elems")
-    if elems.dim() != 2 or elems.shape[1] != K or elems.dtype != torch.uint8 or not elems.is_contiguous():
-        raise ValueError(f"{name}_elems must be a contiguous uint8 tensor [lines, {K}]")
-    lines = elems.shape[0]
-    tile = scales.shape != (lines, K // BLOCK128)
-    _flat(scales, name + "_scales", (-(-lines // BLOCK128), K // BLOCK128) if tile else (lines, K // BLOCK128), torch.float32, elems.device)
+    shape, blocks = elems.shape, K // BLOCK128
+    if len(shape) != 2 or shape[1] != K or elems.dtype != torch.uint8 or elems.get_device() != index or not elems.is_contiguous():
+        raise ValueError(f"{name}_elems must be a contiguous uint8 tensor [lines, {K}] on device {index}")
+    lines, shape_s = shape[0], scales.shape
+    tile = shape_s != (lines, blocks)
+    if tile and shape_s != (-(-lines // BLOCK128), blocks) or scales.dtype != torch.float32 or scales.get_device() != index or not scales.is_contiguous():
+        raise ValueError(f"{name}_scales must be a contiguous float32 tensor [{lines}, {blocks}] or [{-(-lines // BLOCK128)}, {blocks}] on device {index}")
     return lines, tile
 
 
 def mx_gemm_b128(A_elems, A_scales, fmtA, B_elems, B_scales, fmtB, K, dtype=torch.float32, out=None, stream=None):
     """C[M, N] = A[M, K] . B[N, K]^T on operands cast by mx_quantize_b128; which have 128 x 128 tiles is seen from their scales' shapes."""
-    M, tileA = _b128_operand(A_elems, A_scales, "A", K)
-    N, tileB = _b128_operand(B_elems, B_scales, "B", K)
-    if B_elems.device != A_elems.device:
-        raise ValueError("A and B must be on one device")
+    index = _where(A_elems, "A_elems")
+    M, tileA = _b128_operand(A_elems, A_scales, "A", K, index)
+    N, tileB = _b128_operand(B_elems, B_scales, "B", K, index)
     if out is None:
-        out = torch.empty((M, N), dtype=dtype, device=A_elems.device)
-    elif tuple(out.shape) != (M, N) or out.device != A_elems.device or (N > 1 and out.stride(1) != 1):
-        raise ValueError(f"out must be a [{M}, {N}] tensor with contiguous rows on {A_elems.device}")
+        out = _made((M, N), dtype, index)
+    elif out.shape != (M, N) or out.get_device() != index or (N > 1 and out.stride(1) != 1):
+        raise ValueError(f"out must be a [{M}, {N}] tensor with contiguous rows on device {index}")
     ldc = out.stride(0) if M > 1 else N
-    _call(A_elems.device, stream, lib().mx_gemm_b128, M, N, K, A_elems.data_ptr(), A_scales.data_ptr(), tileA, fmtA, B_elems.data_ptr(), B_scales.data_ptr(), tileB, fmtB,
+    _call(index, stream, lib().mx_gemm_b128, M, N, K, A_elems.data_ptr(), A_scales.data_ptr(), tileA, fmtA, B_elems.data_ptr(), B_scales.data_ptr(), tileB, fmtB,
           out.data_ptr(), _dt(out), ldc)
     return out
 
@@ -547,87 +552,94 @@ def mx_gemm_b128(A_elems, A_scales, fmtA, B_elems, B_scales, fmtB, K, dtype=torc
 # RMS norm (include/mx_norm.h)
 # ---------------------------------------------------------------------------------------------
 def _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out):
-    """(the leading arguments of a norm call, the trailing ones)"""
-    ldx = _rows(x, "x")
-    rows, cols = x.shape
-    ldr = _rows(residual, "residual", x) if residual is not None else 0
-    ldh = _rows(h_out, "h_out", x) if h_out is not None else 0
-    ldy = _rows(y_out, "y_out", x) if y_out is not None else 0
-    w_dt = DT_F32
+    """(device index, shape, the leading arguments of a norm call, the trailing ones)"""
+    index, shape, dtype, dt = _where(x, "x"), x.shape, x.dtype, _dt(x)
+    ldx = _rows(x, "x", shape, dtype, index)
+    rows, cols = shape
+    r = h = y = w = rstd = None
+    ldr = ldh = ldy = w_dt = 0
+    if residual is not None:
+        r, ldr = residual.data_ptr(), _rows(residual, "residual", shape, dtype, index)
+    if h_out is not None:
+        h, ldh = h_out.data_ptr(), _rows(h_out, "h_out", shape, dtype, index)
+    if y_out is not None:
+        y, ldy = y_out.data_ptr(), _rows(y_out, "y_out", shape, dtype, index)
     if weight is not None:
-        _flat(weight, "weight", (cols,), weight.dtype, x.device)
         w_dt = _dt(weight)
+        w = _flat(weight, "weight", (cols,), weight.dtype, index).data_ptr()
     if rstd_out is not None:
-        _flat(rstd_out, "rstd_out", (rows,), torch.float32, x.device)
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    return ((x.data_ptr(), ldx, ptr(residual), ldr, ptr(weight), w_dt, _dt(x), rows, cols, float(eps)),
-            (ptr(h_out), ldh, ptr(y_out), ldy, ptr(rstd_out)))
+        rstd = _flat(rstd_out, "rstd_out", (rows,), torch.float32, index).data_ptr()
+    return index, shape, (x.data_ptr(), ldx, r, ldr, w, w_dt, dt, rows, cols, float(eps)), (h, ldh, y, ldy, rstd)
 
 
 def mx_rmsnorm(x, weight, eps, residual=None, h_out=None, y_out=None, rstd_out=None, stream=None):
     """y = h * weight / sqrt(mean(h^2) + eps) per row, h = x + residual, in x's type.  h_out (which may be x or residual) receives h,
     rstd_out ([rows] float32) the factor that mx_rmsnorm_bwd wants.  Returns y."""
     if y_out is None:
-        _rows(x, "x")
-        y_out = _empty_rows(x.shape[0], x.shape[1], x.dtype, x.device)
-    head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
-    _call(x.device, stream, lib().mx_rmsnorm, *head, *tail)
+        index = _where(x, "x")
+        if x.dim() != 2:
+            raise ValueError("x must be a matrix")
+        y_out = _empty_rows(*x.shape, x.dtype, index)
+    index, _, head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
+    _call(index, stream, lib().mx_rmsnorm, *head, *tail)
     return y_out
 
 
 def mx_rmsnorm_q(x, weight, eps, fmt, rnd=ROUND_RNE, residual=None, h_out=None, y_out=None, rstd_out=None, elems_out=None, scales_out=None, stream=None):
     """The norm delivered as an MX tensor blocked along the row: (elems, scales) as mx_quantize(y, 1, fmt, rnd) of the Float32 y."""
-    head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
-    rows, cols = x.shape
+    index, (rows, cols), head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
     blocks = -(-cols // BLOCK)
     width = blocks * BLOCK * (FORMAT_BITS[fmt] if 0 <= fmt < 6 else 8) // 8
-    elems = torch.empty((rows, width), dtype=torch.uint8, device=x.device) if elems_out is None else _flat(elems_out, "elems_out", (rows, width), torch.uint8, x.device)
-    scales = torch.empty((rows, blocks), dtype=torch.uint8, device=x.device) if scales_out is None else _flat(scales_out, "scales_out", (rows, blocks), torch.uint8, x.device)
-    _call(x.device, stream, lib().mx_rmsnorm_q, *head, fmt, rnd, elems.data_ptr(), scales.data_ptr(), *tail)
+    elems = _made((rows, width), torch.uint8, index) if elems_out is None else _flat(elems_out, "elems_out", (rows, width), torch.uint8, index)
+    scales = _made((rows, blocks), torch.uint8, index) if scales_out is None else _flat(scales_out, "scales_out", (rows, blocks), torch.uint8, index)
+    _call(index, stream, lib().mx_rmsnorm_q, *head, fmt, rnd, elems.data_ptr(), scales.data_ptr(), *tail)
     return elems, scales
 
 
 def mx_rmsnorm_b128(x, weight, eps, fmt, residual=None, h_out=None, y_out=None, rstd_out=None, elems_out=None, scales_out=None, stream=None):
     """The norm delivered in 8 bits with a Float32 scale per 128: (elems, scales) as mx_quantize_b128(y, 1, fmt) of the Float32 y."""
-    head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
-    shape_e, shape_s = _b128_shapes(x.shape[0], x.shape[1], 1, False)
-    elems = torch.empty(shape_e, dtype=torch.uint8, device=x.device) if elems_out is None else _flat(elems_out, "elems_out", shape_e, torch.uint8, x.device)
-    scales = torch.empty(shape_s, dtype=torch.float32, device=x.device) if scales_out is None else _flat(scales_out, "scales_out", shape_s, torch.float32, x.device)
-    _call(x.device, stream, lib().mx_rmsnorm_b128, *head, fmt, elems.data_ptr(), scales.data_ptr(), *tail)
+    index, (rows, cols), head, tail = _norm_args(x, weight, eps, residual, h_out, y_out, rstd_out)
+    shape_e, shape_s = _b128_shapes(rows, cols, 1, False)
+    elems = _made(shape_e, torch.uint8, index) if elems_out is None else _flat(elems_out, "elems_out", shape_e, torch.uint8, index)
+    scales = _made(shape_s, torch.float32, index) if scales_out is None else _flat(scales_out, "scales_out", shape_s, torch.float32, index)
+    _call(index, stream, lib().mx_rmsnorm_b128, *head, fmt, elems.data_ptr(), scales.data_ptr(), *tail)
     return elems, scales
 
 
 def mx_rmsnorm_bwd(dy, h, weight, rstd, dh=None, dx_out=None, want_dweight=True, stream=None):
     """Gradients of the norm: (dx, dweight float32 [cols], or None with want_dweight=False).  h and rstd as the forward pass left them; dh, the gradient that
     reaches h by other ways, is added to dx.  dx_out may be dy, h or dh."""
-    ldy = _rows(dy, "dy")
-    rows, cols = dy.shape
-    ldh = _rows(h, "h", dy)
-    lddh = _rows(dh, "dh", dy) if dh is not None else 0
-    w_dt = DT_F32
+    index, shape, dtype, dt = _where(dy, "dy"), dy.shape, dy.dtype, _dt(dy)
+    ldy = _rows(dy, "dy", shape, dtype, index)
+    ldh = _rows(h, "h", shape, dtype, index)
+    rows, cols = shape
+    past = w = None
+    lddh = w_dt = 0
+    if dh is not None:
+        past, lddh = dh.data_ptr(), _rows(dh, "dh", shape, dtype, index)
     if weight is not None:
-        _flat(weight, "weight", (cols,), weight.dtype, dy.device)
         w_dt = _dt(weight)
-    _flat(rstd, "rstd", (rows,), torch.float32, dy.device)
-    dx = _empty_rows(rows, cols, dy.dtype, dy.device) if dx_out is None else dx_out
-    lddx = _rows(dx, "dx_out", dy)
-    dweight = torch.empty((cols,), dtype=torch.float32, device=dy.device) if want_dweight else None
-    ws = _bwd_workspace(rows, cols, dy.device, stream) if want_dweight else None
+        w = _flat(weight, "weight", (cols,), weight.dtype, index).data_ptr()
+    _flat(rstd, "rstd", (rows,), torch.float32, index)
+    dx = _empty_rows(rows, cols, dtype, index) if dx_out is None else dx_out
+    lddx = _rows(dx, "dx_out", shape, dtype, index)
+    dweight = _made((cols,), torch.float32, index) if want_dweight else None
+    ws = _bwd_workspace(rows, cols, index, stream) if want_dweight else None
     wp, wb = _ws_args(ws)
-    _call(dy.device, stream, lib().mx_rmsnorm_bwd_ws, dy.data_ptr(), ldy, h.data_ptr(), ldh, None if weight is None else weight.data_ptr(), w_dt, rstd.data_ptr(),
-          None if dh is None else dh.data_ptr(), lddh, _dt(dy), rows, cols, dx.data_ptr(), lddx, None if dweight is None else dweight.data_ptr(), wp, wb)
+    _call(index, stream, lib().mx_rmsnorm_bwd_ws, dy.data_ptr(), ldy, h.data_ptr(), ldh, w, w_dt, rstd.data_ptr(), past, lddh, dt, rows, cols, dx.data_ptr(), lddx,
+          None if dweight is None else dweight.data_ptr(), wp, wb)
     return dx, dweight
 
 
-def _bwd_workspace(rows, cols, device, stream):
+def _bwd_workspace(rows, cols, index, stream):
     """The partial sums' scratch memory from torch's caching allocator, or None for the library's own: as for the products, on torch's current
     stream only, and not while it is captured."""
-    if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(device.index):
+    if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(index):
         return None
     if torch.cuda.is_current_stream_capturing():
         return None
     need = lib().mx_rmsnorm_bwd_workspace_bytes(rows, cols)
     try:
-        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        return _made(need, torch.uint8, index) if need else None
     except torch.cuda.OutOfMemoryError:
         return None
