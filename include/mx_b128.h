@@ -82,8 +82,8 @@ int mx_dequantize_b128(const void *elems, const float *scales, mx_format_t fmt,
  * results are reproducible.
  * C, c_dt, ldc, alignment as mx_gemm (scales 16-byte aligned too).  rows of C beyond
  * M and columns beyond N are not touched.
- * MX_ERR_UNSUPPORTED: more than 2^22 tiles of C (of 128 x 128 at least), N of 2^27
- * and more with M up to 64, or K of 2^38 and more.
+ * MX_ERR_UNSUPPORTED: more than 2^22 tiles of C (of 128 x 128 at least), N of 2^29
+ * and more with M up to 32, or K of 2^38 and more.
  */
 int mx_gemm_b128(int64_t M, int64_t N, int64_t K,
                  const void *A_elems, const float *A_scales, int tileA, mx_format_t fmtA,

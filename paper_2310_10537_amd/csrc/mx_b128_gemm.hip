@@ -18,7 +18,7 @@ template <int FA, int FB, int CDT, bool ROWS_B, int MB, int NB, int AHEAD>
 static hipError_t launch_few(const Gemm128 &g, hipStream_t st)
 {
     const int64_t gx = (g.N + 16 * NB - 1) / (16 * NB), gy = (g.M + 16 * MB - 1) / (16 * MB);
-    if (gx >= (int64_t)1 << 23) return hipErrorNotSupported;           // (the runtime counts a grid's threads in 32 bits; M is at most 64)
+    if (gx >= (int64_t)1 << 23) return hipErrorNotSupported;           // (the runtime counts a grid's threads in 32 bits; gy is at most 256)
     hipLaunchKernelGGL((gemm128_few_kernel<FA, FB, CDT, ROWS_B, MB, NB, AHEAD>), dim3((unsigned)gx, (unsigned)gy), dim3(512), 0, st, g);
     return hipGetLastError();
 }
@@ -26,8 +26,10 @@ static hipError_t launch_few(const Gemm128 &g, hipStream_t st)
 // Which form.  Measured at K = 4096 with E4M3 operands and 128 x 128 scales of B unless stated (us):
 //   up to 16 rows      eight waves share K.  16 columns a work-group: 1 x 4096 5.2, 1 x 11008 11.4, 16 x 11008 16.5; 64 columns: 12.7, 14.1, 15.9.  Wide
 //                      matrices (28672, K = 8192) give 64 columns work-groups enough, and read A a quarter as often: 16 rows 72 and 56.
-//   up to 32 rows      the same with two fragments of A: 32 x 4096 9.8 with 16 columns, 17.4 with 64, tiles 18.6; 32 x 11008 26.0, 18.4, 19.6.
-//   up to 64 rows      two row groups and 32 columns while the matrix is narrow: 64 x 4096 12.5, tiles 19.0; 64 x 11008 32.9 and 20.1.
+//   one round          (up to 256 work-groups) of few-rows kernels with 16 x 16, 32 x 16 or 32 x 32 entries, the smallest that gives one: 128 x 256 6.9 us, 9.6,
+//                      11.1, tiles of 128 x 128 16.4; 128 x 1024 11.5 (two rounds), 9.9, 11.9, 16.7; 256 x 1024 20.7 (four), 18.0 (two), 12.0, 16.8; K = 16384,
+//                      128 x 256: 21, 31, 40, 65; K = 1024, 512 x 512: 7.3, 6.6, 4.8, 7.7.  Two rounds of 32 x 32 lose: 128 x 4096 23.4, tiles 20.5.
+//   up to 32 rows      beyond that, 32 x 64 entries a work-group: 32 x 11008 18.4, tiles 19.6.
 //   beyond             tiles, of the size whose rounds over the 256 compute units take least: a round of 128 x 128 tiles (K in halves) takes about
 //                      21, of 256 x 128 34, of 256 x 256 55 (1000 x 4096: 24, 32, 45; 2048 x 4096: 44, 37, 46; 4096 x 4096: 88, 70, 59; 512 x 11008: 42, 33, -).
 //   under four blocks  (K up to 384), and K of 2^24 and more, which the tiles' 32-bit offsets do not reach: tiles of four waves.
@@ -35,11 +37,14 @@ template <int FA, int FB, int CDT, bool ROWS_B>
 static hipError_t launch_rows(const Gemm128 &g, hipStream_t st)
 {
     if (g.M <= 16) return g.N < 16384 ? launch_few<FA, FB, CDT, ROWS_B, 1, 1, 4>(g, st) : launch_few<FA, FB, CDT, ROWS_B, 1, 4, 2>(g, st);
-    if (g.M <= 32) return g.N < 8192 ? launch_few<FA, FB, CDT, ROWS_B, 2, 1, 4>(g, st) : launch_few<FA, FB, CDT, ROWS_B, 2, 4, 2>(g, st);
-    if (g.M <= 64 && g.N < 8192) return launch_few<FA, FB, CDT, ROWS_B, 2, 2, 2>(g, st);
+    auto count = [](int64_t n, int b) { const int64_t t = (n + b - 1) / b; return t < (int64_t)1 << 30 ? t : (int64_t)1 << 30; };
+    auto rounds = [&](int bm, int bn) { return (count(g.M, bm) * count(g.N, bn) + 255) / 256; };
+    if (rounds(16, 16) == 1) return launch_few<FA, FB, CDT, ROWS_B, 1, 1, 4>(g, st);
+    if (rounds(32, 16) == 1) return launch_few<FA, FB, CDT, ROWS_B, 2, 1, 4>(g, st);
+    if (rounds(32, 32) == 1) return launch_few<FA, FB, CDT, ROWS_B, 2, 2, 2>(g, st);
+    if (g.M <= 32) return launch_few<FA, FB, CDT, ROWS_B, 2, 4, 2>(g, st);
     const int64_t T = g.K / 128;
     if (T < TILE_MIN_BLOCKS || T >= 1 << 17) return launch_tiles<FA, FB, CDT, ROWS_B, 4, 4, 2, 2>(g, st);
-    auto rounds = [&](int bm, int bn) { return (((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn) + 255) / 256; };
     const int64_t c256 = 55 * rounds(256, 256), c2x1 = 34 * rounds(256, 128), c128 = 21 * rounds(128, 128);
     if (T >= 2 * TILE_MIN_BLOCKS && T % 2 == 0 && c128 < c256 && c128 <= c2x1) return launch_tile<FA, FB, CDT, ROWS_B, 4, 4, 2, 2, 2>(g, st);
     if (c2x1 < c256) return launch_tile<FA, FB, CDT, ROWS_B, 4, 4, 4, 2, 1>(g, st);

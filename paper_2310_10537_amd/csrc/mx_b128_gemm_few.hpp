@@ -1,5 +1,6 @@
 // The product of mx_b128_gemm.hpp for few rows of A, where reading B is all that costs: each byte of B is wanted once, so it goes
-// straight to registers.  A work-group has 16 MB rows and 16 NB columns; its eight waves take an eighth of the blocks along K each, with AHEAD blocks on
+// straight to registers; and for products of so few entries that one round of small work-groups covers them, where the way along K is all that costs.
+// A work-group has 16 MB rows and 16 NB columns; its eight waves take an eighth of the blocks along K each, with AHEAD blocks on
 // their way, and their partial sums are added in a fixed order through LDS.  A load takes 64 consecutive bytes of 16 rows; rows of A that do
 // not exist are not loaded (one row: half of the load path's work).  1 x 11008 x 4096: 11.4 us, 3.9 TB/s of weights; 1 x 28672 x 8192: 48.6 us, 4.8 TB/s.
 #pragma once

@@ -112,7 +112,8 @@ def integer_operand(rows, K, fmt, tile, g):
 
 GEMMS = [(1, 1, 128), (1, 200, 384), (2, 33, 1152), (15, 130, 1024), (16, 16, 2176), (17, 31, 640), (33, 129, 1280), (64, 300, 256), (65, 64, 128),
          (100, 257, 896), (128, 128, 512), (130, 70, 640), (300, 515, 384), (9, 16500, 256), (20, 8200, 384), (30, 8192, 1152), (64, 8200, 1024), (70, 130, 2048),
-         (65, 257, 512), (200, 33000, 640), (257, 129, 1408), (1030, 8200, 768)]
+         (65, 257, 512), (200, 33000, 640), (257, 129, 1408), (1030, 8200, 768), (520, 530, 1024), (545, 1030, 1152), (530, 520, 384), (1030, 300, 640),
+         (128, 1024, 256), (250, 510, 512)]
 
 
 def product_operands(rows_a, rows_b, K, fa, fb, tiles, seed):
@@ -154,7 +155,7 @@ def check_product(mx, a, sa, fa, b, sb, fb, tiles, K):
     return float(err.norm() / want.norm())
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 300, 4096), (7, 129, 11008), (40, 260, 2048), (64, 96, 8192), (200, 333, 1152), (513, 700, 1024)], ids=str)
+@pytest.mark.parametrize("M,N,K", [(1, 300, 4096), (7, 129, 11008), (40, 260, 2048), (64, 96, 8192), (200, 333, 1152), (513, 700, 1024), (300, 300, 4096), (530, 520, 4096), (520, 530, 1152)], ids=str)
 @pytest.mark.parametrize("fa,fb,tiles", [(0, 0, (False, True)), (1, 0, (False, True)), (0, 1, (False, False)), (0, 0, (True, True))], ids=str)
 def test_product_of_cast_data(mx, M, N, K, fa, fb, tiles):
     a, sa = model.quantize(inputs.student_t_f32((M, K), seed=M), 1, fa, tiles[0])
@@ -162,7 +163,7 @@ def test_product_of_cast_data(mx, M, N, K, fa, fb, tiles):
     check_product(mx, a, sa, fa, b, sb, fb, tiles, K)
 
 
-@pytest.mark.parametrize("M,N", [(3, 40), (70, 260), (300, 130)])
+@pytest.mark.parametrize("M,N", [(3, 40), (70, 260), (300, 130), (600, 530)])
 def test_nan_and_infinity_reach_their_entries_only(mx, M, N):
     K = 512
     x, w = np.ones((M, K), np.float32), np.ones((N, K), np.float32)

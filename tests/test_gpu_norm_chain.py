@@ -134,7 +134,7 @@ def test_norms_beyond_32_bits(mx):
     assert torch.equal(dx[-50:], want)
 
 
-@pytest.mark.parametrize("M,N,K", [(70016, 33000, 512), (8, 70016, 65536), (24, 70016, 65536), (100, 70016, 65536), (70016, 200, 65536), (3, 200, 1 << 25), (100, 200, 1 << 25)], ids=str)
+@pytest.mark.parametrize("M,N,K", [(70016, 33000, 512), (8, 70016, 65536), (24, 70016, 65536), (100, 70016, 65536), (70016, 200, 65536), (3, 200, 1 << 25), (100, 200, 1 << 25), (520, 530, 1 << 24)], ids=str)
 def test_products_beyond_32_bits(mx, M, N, K):
     """C or an operand beyond 2^32 bytes, K beyond the tiles' offsets: the last entries, of numbers whose sums are exact."""
     g = torch.Generator(device="cuda").manual_seed(K)

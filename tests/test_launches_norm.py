@@ -42,19 +42,21 @@ T256, T2X1, T128 = (TILE, 4, 8, 4, 2, 1), (TILE, 4, 4, 4, 2, 1), (TILE, 4, 4, 2,
 def test_forms_of_the_product(trace):
     assert form(trace, 1, 4096, 4096) == form(trace, 16, 16383, 4096) == form(trace, 16, 1, 128) == (FEW, 1, 1, 4)
     assert form(trace, 16, 16384, 4096) == (FEW, 1, 4, 2)
-    assert form(trace, 17, 8191, 4096) == form(trace, 32, 512, 128) == (FEW, 2, 1, 4)
-    assert form(trace, 17, 8192, 4096) == (FEW, 2, 4, 2)
-    assert form(trace, 33, 8191, 4096) == form(trace, 64, 4096, 128) == (FEW, 2, 2, 2)
+    # one round of work-groups over 256 compute units, of the smallest that give one
+    assert form(trace, 17, 2048, 4096) == form(trace, 64, 1024, 128) == form(trace, 256, 256, 1 << 24) == form(trace, 4096, 16, 4096) == (FEW, 1, 1, 4)
+    assert form(trace, 17, 2049, 4096) == form(trace, 17, 4096, 4096) == form(trace, 128, 1024, 128) == form(trace, 4096, 32, 4096) == (FEW, 2, 1, 4)
+    assert form(trace, 17, 4097, 4096) == form(trace, 32, 8192, 4096) == form(trace, 64, 4096, 128) == form(trace, 512, 512, 4096) == form(trace, 8192, 32, 4096) == (FEW, 2, 2, 2)
+    assert form(trace, 17, 8193, 4096) == form(trace, 32, 1 << 20, 128) == (FEW, 2, 4, 2)
     for tb in (0, 1):
-        assert form(trace, 33, 8192, 4096, tb) == form(trace, 65, 4096, 4096, tb) == form(trace, 1000, 4096, 4096, tb) == T128
+        assert form(trace, 33, 8191, 4096, tb) == form(trace, 512, 513, 4096, tb) == form(trace, 65, 4096, 4096, tb) == form(trace, 1000, 4096, 4096, tb) == T128
         assert form(trace, 512, 11008, 4096, tb) == form(trace, 2048, 4096, 4096, tb) == T2X1
         assert form(trace, 8192, 11008, 4096, tb) == form(trace, 4096, 4096, 4096, tb) == form(trace, 1000, 11008, 4096, tb) == T256
     # halves of K want at least four blocks each, and as many in the one as in the other
     assert form(trace, 128, 4096, 1024) == T128
     assert form(trace, 128, 4096, 1024 - 128) == form(trace, 128, 4096, 1024 + 128) == form(trace, 128, 4096, 512) == T2X1
     # less than four blocks, or a K that 32-bit offsets of 256 rows do not reach
-    assert form(trace, 128, 4096, 384) == form(trace, 4096, 4096, 128) == form(trace, 128, 256, 1 << 24) == (PLAIN, 4, 4, 2, 2)
-    assert form(trace, 128, 256, (1 << 24) - 256) == T128
+    assert form(trace, 128, 4096, 384) == form(trace, 4096, 4096, 128) == form(trace, 128, 4096, 1 << 24) == (PLAIN, 4, 4, 2, 2)
+    assert form(trace, 128, 4096, (1 << 24) - 256) == T128
 
 
 def test_formats_and_types_of_the_product(trace):
@@ -62,7 +64,7 @@ def test_formats_and_types_of_the_product(trace):
         for fb in (E4M3, E5M2):
             for dt in (F32, BF16):
                 for tb in (0, 1):
-                    seen = one(trace, *product(300, 500, 1024, tb, fa, fb, dt))
+                    seen = one(trace, *product(600, 500, 1024, tb, fa, fb, dt))
                     assert seen[0][1][:4] == (str(fa), str(fb), str(dt), "false" if tb else "true")
 
 
