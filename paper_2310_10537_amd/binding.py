@@ -632,11 +632,9 @@ def mx_rmsnorm_bwd(dy, h, weight, rstd, dh=None, dx_out=None, want_dweight=True,
 
 
 def _bwd_workspace(rows, cols, index, stream):
-    """The partial sums' scratch memory from torch's caching allocator, or None for the library's own: as for the products, on torch's current
-    stream only, and not while it is captured."""
+    """The partial sums' scratch memory from torch's caching allocator on torch's current stream (while it is captured, from the graph's own pool, like
+    the results: graphs that are replayed at the same time do not share it), else None, for the library's own."""
     if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(index):
-        return None
-    if torch.cuda.is_current_stream_capturing():
         return None
     need = lib().mx_rmsnorm_bwd_workspace_bytes(rows, cols)
     try:

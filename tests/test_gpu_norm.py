@@ -246,3 +246,55 @@ def test_stream_and_captured_graph(mx):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
     del ws
+
+
+def test_two_captured_graphs_at_once(mx):
+    """Gradients captured in two graphs, replayed on two streams at the same time: each has its scratch memory."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = torch.randn((2048,), device="cuda", generator=g)
+    sets, graphs, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for k in range(2):
+        dy, h = (torch.randn((3000, 2048), device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+        rstd = torch.rand((3000,), device="cuda", generator=g) + 0.5
+        sets.append((dy, h, rstd, [t.clone() for t in mx.mx_rmsnorm_bwd(dy, h, w, rstd)]))
+    torch.cuda.synchronize()
+    for dy, h, rstd, _ in sets:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            graphs.append((graph, mx.mx_rmsnorm_bwd(dy, h, w, rstd)))
+    for _ in range(4):
+        for graph, (dx, dw) in graphs:
+            dx.zero_()
+            dw.zero_()
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for st, (graph, _) in zip(streams, graphs):
+                with torch.cuda.stream(st):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for (_, got), (*_, want) in zip(graphs, sets):
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_binding_refuses_tensors_that_do_not_fit(mx):
+    x = torch.zeros((32, 256), device="cuda")
+    w, rstd = torch.ones((256,), device="cuda"), torch.ones((32,), device="cuda")
+    e, s = mx.mx_quantize_b128(x, 1, 0)
+    half = x.to(torch.bfloat16)
+    for call in (lambda: mx.mx_rmsnorm(x[0], w, EPS), lambda: mx.mx_rmsnorm(x.t(), w[:32].contiguous(), EPS), lambda: mx.mx_rmsnorm(x, w[:128], EPS),
+                 lambda: mx.mx_rmsnorm(x, w, EPS, residual=half), lambda: mx.mx_rmsnorm(x, w, EPS, residual=x[:31]), lambda: mx.mx_rmsnorm(x, w, EPS, h_out=x.cpu()),
+                 lambda: mx.mx_rmsnorm(x, w.cpu(), EPS), lambda: mx.mx_rmsnorm(x, w, EPS, rstd_out=rstd.double()), lambda: mx.mx_rmsnorm_q(x, w, EPS, 0, elems_out=e[:, :128]),
+                 lambda: mx.mx_rmsnorm_b128(x, w, EPS, 0, scales_out=s.t()), lambda: mx.mx_rmsnorm_bwd(x, half, w, rstd), lambda: mx.mx_rmsnorm_bwd(x, x, w, rstd[:31]),
+                 lambda: mx.mx_rmsnorm_bwd(x, x, w, rstd, dx_out=x[:, :128]), lambda: mx.mx_dequantize_b128(e, s, 0, 32, 384, 1), lambda: mx.mx_dequantize_b128(e, s, 0, 33, 256, 1),
+                 lambda: mx.mx_dequantize_b128(e, s, 0, 32, 256, 1, out=x[:31]), lambda: mx.mx_gemm_b128(e, s, 0, e, s[:7], 0, 256), lambda: mx.mx_gemm_b128(e, s, 0, e, s, 0, 128),
+                 lambda: mx.mx_gemm_b128(e, s, 0, e.cpu(), s.cpu(), 0, 256), lambda: mx.mx_gemm_b128(e, s, 0, e, s, 0, 256, out=x)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: mx.mx_rmsnorm(x.half(), None, EPS), lambda: mx.mx_rmsnorm(x, w.half(), EPS), lambda: mx.mx_quantize_b128(x.double(), 1, 0),
+                 lambda: mx.mx_gemm_b128(e, s, 0, e, s, 0, 256, dtype=torch.float16)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: mx.mx_quantize_b128(x, 1, 2), lambda: mx.mx_quantize_b128(x, 2, 0), lambda: mx.mx_rmsnorm(x, w, -1.0), lambda: mx.mx_rmsnorm_q(x, w, EPS, 6),
+                 lambda: mx.mx_rmsnorm_q(x, w, EPS, 0, rnd=3), lambda: mx.mx_quantize_b128(torch.zeros((32, 250), device="cuda"), 1, 0)):
+        with pytest.raises(mx.MxError):
+            call()
