@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_half_kernel(int64_t K, const
     auto stage_one = [&](int k, int t, int dst) __attribute__((always_inline)) {
         t = t < T ? t : T - 1;
         const uint8_t *gp = (k < NJA ? gA + k * 32 * row : gB + (k - NJA) * 32 * row) + (int64_t)t * STEP;
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gp), "s"(lds0 + dst + k * 4096) : "m0", "memory");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gp), "s"(lds0 + dst + k * 4096) : "m0", "memory");
     };
     // operand reads: tile row wm*128 + 16x + i (A) / wn*64 + 16y + i (B), chunks q and q + 4: the first and the second 32 elements
     const int ra = (wm * 128 + i) * STEP + ((q ^ ((i >> 1) & 7)) << 4);

@@ -109,10 +109,10 @@ __global__ __launch_bounds__(256, 2) void gemm_mid_kernel(int M, int N, int64_t 
         const uint32_t l = lds0 + dst + k * 4096;
         if (k < NJA) {
             const uint8_t *p = gA + (int64_t)t * (TK * WA / 8);
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(oa[k < NJA ? k : 0]), "s"(p), "s"(l) : "m0", "memory");
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(oa[k < NJA ? k : 0]), "s"(p), "s"(l) : "m0", "memory");
         } else {
             const uint8_t *p = gB + (int64_t)t * (TK * WB / 8);
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(ob[k < NJA ? 0 : k - NJA]), "s"(p), "s"(l) : "m0", "memory");
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(ob[k < NJA ? 0 : k - NJA]), "s"(p), "s"(l) : "m0", "memory");
         }
     };
 
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256, 2) void gemm_mid_kernel(int M, int N, int64_t 
         if (direct_scales) {
             const uint32_t l = scl0 + (G & 1) * SG_BYTES + seg * 1024;
             const uint8_t *p = srow + (4 * G + 4 <= steps ? 16 * G : 4 * steps - 16);
-            asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(l) : "m0", "memory");
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(l) : "m0", "memory");
         } else {
             uint32_t d[4];
             load_scale_group(srow, 16 * (int64_t)G, nkb, d);

@@ -189,11 +189,11 @@ __global__ __launch_bounds__(256, 1) void gemm_tile16_kernel(int64_t M, int64_t 
     // (dst: byte offset of the destination tile inside the LDS array)
     auto stage_a1 = [&](int ts, int dst, int j) {
         const uint8_t *gp = gA + (int64_t)ts * TK + j * (4 * TF::RPI) * K;
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gp), "s"(lds0 + dst + j * 4096) : "m0");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gp), "s"(lds0 + dst + j * 4096) : "m0");
     };
     auto stage_b1 = [&](int ts, int dst, int j) {
         const uint8_t *gp = gB + (int64_t)ts * TK + j * (4 * TF::RPI) * K;
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gp), "s"(lds0 + dst + j * 4096) : "m0");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gp), "s"(lds0 + dst + j * 4096) : "m0");
     };
     // direct load number k of a stage: A's eight, then B's eight
     auto stage_one = [&](int k, int ts, int dstA, int dstB) {
@@ -216,8 +216,8 @@ __global__ __launch_bounds__(256, 1) void gemm_tile16_kernel(int64_t M, int64_t 
         const uint32_t l0 = lds0 + 2 * STAGE_BYTES + (G & 1) * SG_BYTES + wave * (64 * SG_ROW - 1024) + j * 1024;   // lds0 holds wave * 1024
         const int64_t src_ofs = (G * SG + SG <= T ? (int64_t)G * SG_ROW : (int64_t)T * 4 - SG_ROW) + j * 32 * nkb;
         const uint8_t *pa = sA + src_ofs, *pb = sB + src_ofs;
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(pa), "s"(l0) : "m0");
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(pb), "s"(l0 + TM * SG_ROW) : "m0");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(pa), "s"(l0) : "m0");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(pb), "s"(l0 + TM * SG_ROW) : "m0");
     };
     // fragment of 16-row block xb of the tile at buf
     auto frag = [&](const uint8_t *buf, int ofs, int xb) {

@@ -164,8 +164,8 @@ __global__ __launch_bounds__(256, 1) void gemm_tile16_kernel(int64_t M, int64_t 
         const uint32_t vo = vs + 16 * u;
         const uint8_t *pa = sA + set * 32 * nkb, *pb = sB + set * 32 * nkb;
         const uint32_t l0 = lds0 + wave * 2048 + set * 1024;
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(pa), "s"(l0) : "m0");
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(pb), "s"(l0 + 8192) : "m0");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(pa), "s"(l0) : "m0");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(pb), "s"(l0 + 8192) : "m0");
     };
 
     v4f_t acc[8][8];

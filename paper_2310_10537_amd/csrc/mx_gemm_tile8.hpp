@@ -107,13 +107,13 @@ __global__ __launch_bounds__(64 * NW8, 1) void gemm_tile8_kernel(int64_t M, int6
         const uint32_t l0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t *)(dst + st_l));
         const uint8_t *sp = WA == 6 ? sA + (int64_t)ts * (TK * WA / 8) : sA + (int64_t)ts * (TK * WA / 8) + j * (NW8 * TA::RPI) * a_row_bytes;
         const uint32_t vo = WA == 6 ? a6[j < N6A ? j : 0] : vA;
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(sp), "s"(l0 + j * (NW8 * 1024)) : "m0");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(sp), "s"(l0 + j * (NW8 * 1024)) : "m0");
     };
     auto stage_b1 = [&](int ts, uint8_t *dst, int j) {
         const uint32_t l0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t *)(dst + st_l));
         const uint8_t *sp = WB == 6 ? sB + (int64_t)ts * (TK * WB / 8) : sB + (int64_t)ts * (TK * WB / 8) + j * (NW8 * TB::RPI) * b_row_bytes;
         const uint32_t vo = WB == 6 ? b6[j < N6B ? j : 0] : vB;
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(sp), "s"(l0 + j * (NW8 * 1024)) : "m0");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(sp), "s"(l0 + j * (NW8 * 1024)) : "m0");
     };
     auto stage_all = [&](int ts, uint8_t *dst) {
 #pragma unroll
@@ -143,10 +143,10 @@ __global__ __launch_bounds__(64 * NW8, 1) void gemm_tile8_kernel(int64_t M, int6
         const uint32_t l0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t *)(dst + wave * 1024));
         const int64_t src_ofs = G * SCL_GROUP + SCL_GROUP <= T ? (int64_t)G * 16 : (int64_t)T * 4 - 16;
         const uint8_t *p = sS0 + src_ofs;
-        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vS), "s"(p), "s"(l0) : "m0");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vS), "s"(p), "s"(l0) : "m0");
         if (NW8 < N_SCL && wave + NW8 < N_SCL) {            // wave-uniform
             const uint8_t *p1 = sS1 + src_ofs;
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vS), "s"(p1), "s"(l0 + NW8 * 1024) : "m0");
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vS), "s"(p1), "s"(l0 + NW8 * 1024) : "m0");
         }
     };
     // Scale bytes.  A row's 16-byte LDS slot holds the dwords of the four K steps of a scale group.  Reading
