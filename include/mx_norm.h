@@ -70,6 +70,10 @@ int mx_rmsnorm_b128(const void *x, int64_t ldx, const void *residual, int64_t ld
  * `workspace` (16-byte aligned; too small: MX_ERR_WORKSPACE; NULL: as the plain
  * form).  The order of every sum depends on the shape alone.  rows = 0 with a
  * dweight writes zeros.
+ * While hip_stream is captured, memory from the pool becomes an allocation and a
+ * release inside the graph, and what two graphs that run at the same time get is for
+ * the runtime to say: such graphs want the _ws form with a workspace each, which
+ * has to stay theirs for as long as they are replayed.
  */
 size_t mx_rmsnorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
 int mx_rmsnorm_bwd(const void *dy, int64_t lddy, const void *h, int64_t ldh,

@@ -608,7 +608,8 @@ def mx_rmsnorm_b128(x, weight, eps, fmt, residual=None, h_out=None, y_out=None, 
 
 def mx_rmsnorm_bwd(dy, h, weight, rstd, dh=None, dx_out=None, want_dweight=True, stream=None):
     """Gradients of the norm: (dx, dweight float32 [cols], or None with want_dweight=False).  h and rstd as the forward pass left them; dh, the gradient that
-    reaches h by other ways, is added to dx.  dx_out may be dy, h or dh."""
+    reaches h by other ways, is added to dx.  dx_out may be dy, h or dh.  (Of a captured call dweight is the front of a piece of memory that holds the
+    graph's scratch memory too.)"""
     index, shape, dtype, dt = _where(dy, "dy"), dy.shape, dy.dtype, _dt(dy)
     ldy = _rows(dy, "dy", shape, dtype, index)
     ldh = _rows(h, "h", shape, dtype, index)
@@ -623,21 +624,35 @@ def mx_rmsnorm_bwd(dy, h, weight, rstd, dh=None, dx_out=None, want_dweight=True,
     _flat(rstd, "rstd", (rows,), torch.float32, index)
     dx = _empty_rows(rows, cols, dtype, index) if dx_out is None else dx_out
     lddx = _rows(dx, "dx_out", shape, dtype, index)
-    dweight = _made((cols,), torch.float32, index) if want_dweight else None
-    ws = _bwd_workspace(rows, cols, index, stream) if want_dweight else None
+    dweight, ws = _bwd_dweight(rows, cols, index, stream) if want_dweight else (None, None)
     wp, wb = _ws_args(ws)
     _call(index, stream, lib().mx_rmsnorm_bwd_ws, dy.data_ptr(), ldy, h.data_ptr(), ldh, w, w_dt, rstd.data_ptr(), past, lddh, dt, rows, cols, dx.data_ptr(), lddx,
           None if dweight is None else dweight.data_ptr(), wp, wb)
     return dx, dweight
 
 
-def _bwd_workspace(rows, cols, index, stream):
-    """The partial sums' scratch memory from torch's caching allocator on torch's current stream (while it is captured, from the graph's own pool, like
-    the results: graphs that are replayed at the same time do not share it), else None, for the library's own."""
-    if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(index):
-        return None
+def _captured(index, stream):
+    """Whether the work of a call (on `stream`, else torch's current one of that device) goes into a graph."""
+    if index == torch._C._cuda_getDevice() and (stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(index)):
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.device(index), torch.cuda.stream(None if stream is None else torch.cuda.ExternalStream(stream.cuda_stream, device=index)):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _bwd_dweight(rows, cols, index, stream):
+    """dweight and the partial sums' scratch memory.  On torch's current stream that comes from torch's caching allocator, on another one it is None, for the
+    library's own, in that stream's order.  A captured call runs with every replay, long after a tensor dropped here would have gone back to
+    the allocator (which only torch's own captures keep apart): there it lies behind dweight, in the same piece of memory, and lives as long as that.  So graphs that are
+    replayed at the same time do not share it either."""
     need = lib().mx_rmsnorm_bwd_workspace_bytes(rows, cols)
+    if need and _captured(index, stream):
+        ahead = -(-4 * cols // 256) * 256
+        both = _made((ahead + need,), torch.uint8, index)
+        return both[:4 * cols].view(torch.float32), both[ahead:]
+    dweight = _made((cols,), torch.float32, index)
+    if not need or (stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(index)):
+        return dweight, None
     try:
-        return _made(need, torch.uint8, index) if need else None
+        return dweight, _made((need,), torch.uint8, index)
     except torch.cuda.OutOfMemoryError:
-        return None
+        return dweight, None
