@@ -149,14 +149,14 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_bwd_kernel(NormBwdArgs
     for (int k = 0; k < VPT; k++) {
         const int64_t col = (int64_t)(k * nt + t) * 8;
         const int n = inside(a.cols - col, 8);
-        if constexpr (WAVE) {                         // four rows at a time: their waves' sums in order
+        if constexpr (WAVE) {                         // four rows at a time: their waves' sums in pairs
 #pragma unroll
             for (int i = 0; i < 8; i++) lds[threadIdx.x * 8 + i] = dw[k][i];
             __syncthreads();
             if (threadIdx.x < 64) {
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const float v = ((lds[t * 8 + i] + lds[(64 + t) * 8 + i]) + lds[(128 + t) * 8 + i]) + lds[(192 + t) * 8 + i];
+                    const float v = (lds[t * 8 + i] + lds[(64 + t) * 8 + i]) + (lds[(128 + t) * 8 + i] + lds[(192 + t) * 8 + i]);
                     if (i < n) line[col + i] = v;
                 }
             }
@@ -168,31 +168,30 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_bwd_kernel(NormBwdArgs
     }
 }
 
-// dweight[c] = partial[0][c] + partial[1][c] + ..., 16 columns and 64 runs of lines a work-group
+// dweight[c] = partial[0][c] + partial[1][c] + ..., 16 columns and 64 runs of lines (every 64th) a work-group
 __global__ __launch_bounds__(1024) void norm_bwd_weight_kernel(const float *__restrict__ partial, int lines, int64_t pitch, int64_t cols, float *__restrict__ dweight)
 {
     __shared__ float part[64][17];
     const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
     const int64_t col = (int64_t)blockIdx.x * 16 + c;
+    // eight lines of a run at a time, and then the 64 runs, joined in pairs, and these in pairs: eleven roundings at most up to 1024 lines
+    // (333 x 1000 Float32, Gaussian: dweight's error 1.7e-7 of it and 8.1 us for both kernels with everything one after the other, 8.8e-8 and 7.0 so)
     float sum = 0.0f;
     if (col < cols) {
-        int l = g;
-        for (; l + 448 < lines; l += 512) {
+        for (int l = g; l < lines; l += 512) {
             float v[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) v[j] = partial[(int64_t)(l + 64 * j) * pitch + col];
-#pragma unroll
-            for (int j = 0; j < 8; j++) sum += v[j];
+            for (int j = 0; j < 8; j++) v[j] = l + 64 * j < lines ? partial[(int64_t)(l + 64 * j) * pitch + col] : 0.0f;
+            sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
-        for (; l < lines; l += 64) sum += partial[(int64_t)l * pitch + col];
     }
     part[g][c] = sum;
-    __syncthreads();
-    if (threadIdx.x < 16 && col < cols) {
-        sum = 0.0f;
-        for (int j = 0; j < 64; j++) sum += part[j][c];
-        dweight[col] = sum;
+#pragma unroll
+    for (int n = 16; n > 0; n >>= 2) {
+        __syncthreads();
+        if (g < n) part[g][c] = (part[g][c] + part[g + n][c]) + (part[g + 2 * n][c] + part[g + 3 * n][c]);
     }
+    if (g == 0 && col < cols) dweight[col] = part[0][c];
 }
 
 template <int DT>
