@@ -6,7 +6,9 @@
  *     h    = x + residual, rounded to the tensors' type (h = x without a residual)
  *     rstd = 1 / sqrt(mean of h^2 over the row + eps)
  *     y    = h * weight * rstd in Float32 (weight NULL: 1)
- * Sums are Float32: a row whose sum of squares passes Float32's range has rstd 0.
+ * Sums are Float32: a row whose sum of squares passes Float32's range has rstd 0 (and y
+ * zero, or NaN where h or h * weight is infinite).  With eps = 0 a row of zeros, or of
+ * numbers whose squares vanish in Float32, has rstd infinity, and its zeros give NaN.
  *
  * Common arguments
  *   x, ldx              [rows, cols] of type dt, rows ldx elements apart

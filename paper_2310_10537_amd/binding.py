@@ -3,6 +3,10 @@
 Argument marshalling only: every step of the cast, the dequantize and the GEMM
 runs in the HIP kernels of the library.  PyTorch is used for device memory and
 for the current stream.  There is no fallback: a missing library is an error.
+
+`stream`: the stream that a call's work is put on, torch's current one without it.  With another one its order is the caller's:
+results made here are torch memory of the current stream, so that stream has to wait for the current one before the call
+(`stream.wait_stream`), and whoever uses or drops the tensors before the work is done waits for it, or tells torch (`Tensor.record_stream`).
 """
 import ctypes
 import os

@@ -25,12 +25,14 @@ static hipError_t launch_few(const Gemm128 &g, hipStream_t st)
 
 // Which form.  Measured at K = 4096 with E4M3 operands and 128 x 128 scales of B unless stated (us):
 //   up to 16 rows      eight waves share K.  16 columns a work-group: 1 x 4096 5.2, 1 x 11008 11.4, 16 x 11008 16.5; 64 columns: 12.7, 14.1, 15.9.  Wide
-//                      matrices (28672, K = 8192) give 64 columns work-groups enough, and read A a quarter as often: 16 rows 72 and 56.
+//                      matrices (28672, K = 8192) give 64 columns work-groups enough, and read A a quarter as often: 16 rows 72 and 56-62.  The rule looks at N
+//                      alone, so at 16 x 11008 it takes the form that is 4 % behind, for the sake of the one row that is 10 % ahead.
 //   one round          (up to 256 work-groups) of few-rows kernels with 16 x 16, 32 x 16 or 32 x 32 entries, the smallest that gives one: 128 x 256 6.9 us, 9.6,
 //                      11.1, tiles of 128 x 128 16.4; 128 x 1024 11.5 (two rounds), 9.9, 11.9, 16.7; 256 x 1024 20.7 (four), 18.0 (two), 12.0, 16.8; K = 16384,
 //                      128 x 256: 21, 31, 40, 65; K = 1024, 512 x 512: 7.3, 6.6, 4.8, 7.7.  Two rounds of 32 x 32 lose: 128 x 4096 23.4, tiles 20.5.
-//   up to 32 rows      beyond that, 32 x 64 entries a work-group: 32 x 11008 18.4, tiles 19.6.
-//   beyond             tiles, of the size whose rounds over the 256 compute units take least: a round of 128 x 128 tiles (K in halves) takes about
+//   up to 32 rows      beyond that, 32 x 64 entries a work-group: 32 x 11008 18.4, tiles 19.6.  With a scale a row of B 27.7: the 32 scales of a block on its way
+//                      spill 30 registers (124 bytes a lane).
+//   beyond             tiles, of the size whose rounds over the 256 compute units take least: a round of 128 x 128 tiles (K in halves, of as many blocks each) takes about
 //                      21, of 256 x 128 34, of 256 x 256 55 (1000 x 4096: 24, 32, 45; 2048 x 4096: 44, 37, 46; 4096 x 4096: 88, 70, 59; 512 x 11008: 42, 33, -).
 //   under four blocks  (K up to 384), and K of 2^24 and more, which the tiles' 32-bit offsets do not reach: tiles of four waves.
 template <int FA, int FB, int CDT, bool ROWS_B>

@@ -5,7 +5,7 @@
 // of 2 x 2 waves, 64 x 64 entries each, half of K each: as many waves a tile where there are few tiles).
 // The scaling of the partial sums is vector work, 4 instructions of 4 clocks beside each matrix instruction of 32, and a wave issues an
 // instruction about every 5 clocks, so one wave on a SIMD cannot issue all that a matrix instruction wants beside it (four waves of 96 x 128 entries, operands in
-// accumulation registers: 383 us for 8192 x 11008 x 4096, 351 for 2048 x 8192 x 16384 with a scale a column; eight waves: 331-339 and 264-271).  With two, one
+// accumulation registers: 383 us for 8192 x 11008 x 4096, 351 for 2048 x 8192 x 16384 with a scale a column; eight waves: 324-341 and 262-278).  With two, one
 // wave's vector work runs under the other's matrix instructions: alone on a SIMD, two waves take 33 clocks for a matrix instruction with four multiply-adds,
 // 46 with eight (a matrix instruction keeps the vector pipe from others for about 14 clocks), so with a scale a column of B the vector work is the bound.
 // What is left is power: the clock is at 1.8 to 1.9 GHz, and on operands of zeros the two products take 275 and 225 us.  Lines fetched into the L2 two steps ahead

@@ -3,13 +3,14 @@
 // delivered as any of: h, y in the tensors' type, rstd, and the cast of the Float32 y to an MX format or to 8 bits with a
 // Float32 scale per 128.  (h w first: for bf16 h and w that product is exact, so y carries one rounding and that of rstd.)
 // Bound by memory: x and the residual read, h and the codes written, all once.  8192 x 4096 bf16 with a residual: 45.1 us with a Float32 scale per 128
-// (5.2 TB/s), MX E4M3 42.7, E2M1 39.8, E3M2 54.2 (its converts want a whole block in a lane, so the exact encoder packs it); one row of 4096 2.8.
+// (5.2 TB/s), MX E4M3 42.7-44.9, E2M1 39.8, E3M2 54-56 (its converts want a whole block in a lane, so the exact encoder packs it); one row of 4096 2.8.
 //
 // norm_kernel: a row stays in registers between the sum of squares and the output: a vector of eight elements a thread and as many threads as
 // that takes, two vectors beyond 8192 columns, and for up to 512 columns a wave a row, four rows a work-group.  More vectors a thread and
 // fewer threads are slower throughout: 8192 x 4096 bf16 with a residual 44 us with one (512 threads), 45 with two, 48 with four, 58 with eight
 // (a wave a row); one row of 4096 3.0, 3.9, 5.6 and 8.9; 2048 x 16384 46 with two vectors, 48 with four, 57 with eight.
-// norm_long_kernel: rows beyond 16384 columns; h is read (or added up) a second time.
+// norm_long_kernel: rows beyond 16384 columns; h is read (or added up) a second time.  1024 x 32768 bf16 with a residual 53 us (4.4 TB/s of what has to be
+// moved), 64 x 131072 42: a work-group a row leaves most compute units without one.
 #pragma once
 
 #include "mx_norm.hpp"
