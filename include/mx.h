@@ -311,7 +311,8 @@ int mx_gemm_qa(int64_t M, int64_t N, int64_t K,
  * and where the memory pool has no room for an MX_INT8 product of other sizes than
  * whole 256 x 256 tiles, which then runs on the integer kernels (a different Float32
  * rounding).  Otherwise results are bit-identical between the two forms.  A call
- * captured into a graph without a workspace puts the allocation into the graph.
+ * captured into a graph without a workspace puts the allocation into the graph;
+ * graphs that run at the same time want a workspace each.
  */
 size_t mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, mx_format_t fmtA, mx_format_t fmtB);
 size_t mx_gemm_qa_workspace_bytes(int64_t M, int64_t N, int64_t K, mx_format_t fmtA, mx_format_t fmtB);

@@ -639,6 +639,8 @@ def _captured(index, stream):
     """Whether the work of a call (on `stream`, else torch's current one of that device) goes into a graph."""
     if index == torch._C._cuda_getDevice() and (stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(index)):
         return torch.cuda.is_current_stream_capturing()
+    if stream is not None and not stream.cuda_stream:
+        return False                                  # the null stream: it is never captured, and torch makes a stream of its own of a handle that is zero
     with torch.cuda.device(index), torch.cuda.stream(None if stream is None else torch.cuda.ExternalStream(stream.cuda_stream, device=index)):
         return torch.cuda.is_current_stream_capturing()
 

@@ -87,3 +87,10 @@ def test_none_without_a_weight_gradient_or_rows(call):
         assert call(100, 1000, want_dweight=False, capture=capture)[1:] == (None, 0)
         dw, pointer, size = call(0, 1000, capture=capture)
         assert dw.shape == (1000,) and pointer is None and size == 0
+
+
+def test_the_null_stream_is_never_captured(call, monkeypatch):
+    """(torch makes a stream of its own of a handle that is zero.)"""
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda raw, device=None: OTHER)
+    dw, pointer, size = call(333, 1000, stream=types.SimpleNamespace(cuda_stream=0), capture=(OTHER,))
+    assert pointer is None and size == 0 and whole(dw)[1] - whole(dw)[0] == 4000
